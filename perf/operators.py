@@ -262,8 +262,11 @@ def _plain_place(state):
     return {"y": y.to(dtype), "dx": dx.to(dtype), "dlogits": dlogits, "dw1": dw1.to(dtype), "db1": db1, "dw2": dw2.to(dtype), "db2": db2}
 
 
-# The 8-bit states: blocks of 256 elements with the largest magnitude s as their scale; first averages as
-# s * (c/127) * |c/127| with c in -127..127, second averages as s * (c/255)^4 with c in 0..255, 0 only for 0.
+# The 8-bit states: blocks of 256 elements with the largest magnitude s as their scale (0 where it is no normal number);
+# first averages as s (c/127) |c/127| with c in -127..127, second averages as s (c/255)^4 with c in 0..255, 0 only for 0.
+# A code is the whole number whose borders c - 1/2 and c + 1/2, squared (to the fourth), hold the scaled value between them.
+
+SMALLEST = 2.0 ** -126
 
 
 def _blocks(x):
@@ -273,18 +276,32 @@ def _blocks(x):
     return padded.view(-1, BLOCK)
 
 
+def _scaled(magnitude, most):
+    """(scale of every block, magnitudes with the scale at `most`)."""
+    s = magnitude.amax(1)
+    s = torch.where(s < SMALLEST, 0.0, s)
+    factor = torch.where(s > 0, torch.full_like(s, most) / torch.where(s > 0, s, 1.0), 0.0)
+    return s, magnitude * factor[:, None]
+
+
 def _encode_first(m):
     b = _blocks(m)
-    s = b.abs().amax(1)
-    c = torch.round(torch.sqrt(b.abs() / torch.where(s > 0, s, 1.0)[:, None]) * 127.0)
+    s, t = _scaled(b.abs(), 127.0 ** 2)
+    c = torch.round(torch.sqrt(t))
+    up, down = c + 0.5, c - 0.5
+    c = c + (t >= up * up).float() - (t < down * down).float() * (c > 0)
     return (torch.sign(b) * c).view(-1)[:m.numel()].to(torch.int8), s
 
 
 def _encode_second(v):
     b = _blocks(v)
-    s = b.amax(1)
-    c = torch.round(torch.sqrt(torch.sqrt(b / torch.where(s > 0, s, 1.0)[:, None])) * 255.0)
-    return torch.where(b > 0, c.clamp(min=1.0), 0.0).view(-1)[:v.numel()].to(torch.uint8), s
+    s, t = _scaled(b, 255.0 ** 4)
+    c = torch.round(torch.sqrt(torch.sqrt(t)))
+    up, down = c + 0.5, c - 0.5
+    up, down = up * up, down * down
+    c = c + (t >= up * up).float() - (t < down * down).float() * (c > 0)
+    c = torch.where((b > 0) & (s > 0)[:, None], c.clamp(min=1.0), 0.0)
+    return c.view(-1)[:v.numel()].to(torch.uint8), s
 
 
 def _decode_first(codes, s):
