@@ -523,6 +523,179 @@ int nomad_random_triplet_accuracy_noalloc(const float* X, int64_t n, int32_t d, 
 int nomad_pca_init(const float* X, int64_t n, int32_t d, float std0, float* theta_out, double* stats, int mem, int32_t device,
                    void* stream);
 
+/*
+ * ---- operators of a learned map: router, products grouped by expert, weighted sum, AdamW ----
+ *
+ * A map that has been fitted is a table of points; these are the operators of a function that places new vectors on it:
+ * every region of the partition has an expert, a router chooses a row's experts, their products run over ragged groups of
+ * rows, and AdamW fits them.  They follow no passage of the paper.
+ *
+ * Conventions of these calls: all arrays are device memory of `device`; a call checks its arguments on the host (sizes,
+ * types, strides, pointers, not what device arrays hold), enqueues its kernels on `stream` and returns without waiting; it
+ * allocates nothing (work space is the caller's, of the size that the *_workspace function names) and copies nothing to or
+ * from the host, so it can be recorded into a HIP graph.  Strides are in elements.  Results do not depend on timing: no atomics on
+ * floating-point numbers.  Sums are held in float32.  Errors: NOMAD_E_INVALID_ARG, NOMAD_E_TOO_LARGE, NOMAD_E_HIP.
+ */
+#define NOMAD_F32 0
+#define NOMAD_BF16 1
+#define NOMAD_F16 2
+
+#define NOMAD_ACT_NONE 0
+#define NOMAD_ACT_RELU 1
+#define NOMAD_ACT_SILU 2 /* z / (1 + e^-z)                     */
+#define NOMAD_ACT_GELU 3 /* z (1 + erf(z / sqrt 2)) / 2        */
+
+#define NOMAD_MAX_ROWS 2147483392    /* rows times k of a call          */
+#define NOMAD_MAX_COLUMNS 1048576
+#define NOMAD_MAX_GROUPS 1048576
+#define NOMAD_ROUTE_MAX_EXPERTS 16384
+#define NOMAD_ROUTE_MAX_K 8
+
+/*
+ * The k best experts of every row and the rows in the order of their experts.
+ *
+ *   logits     [n, n_experts] of `dtype`, rows `stride` apart; 1 <= k <= min(NOMAD_ROUTE_MAX_K, n_experts)
+ *   experts    [n, k] int32 out: the k largest logits of the row in descending order, ties to the lower expert; -1 where
+ *              there is none: an expert with a logit of -inf (a mask) or NaN is never chosen
+ *   weights    [n, k] fp32 out: e^l over the sum of e^l of the row's chosen (normalize = 1) or of all its experts (0); 0
+ *              beside a -1.  A logit of +inf makes the row's weights NaN, as it does a softmax
+ *   offsets    [n_experts + 1] int32 out: expert e has places offsets[e] .. offsets[e+1] - 1
+ *   order      [n k] int32 out: the slots (row times k plus rank) by expert, ascending within one; -1 from
+ *              offsets[n_experts] on
+ *   slots      [n, k] int32 out: the place of every slot in that order, or -1
+ *
+ * NaN aside, all integers are exact.  n = 0 gives empty groups.
+ */
+int64_t nomad_route_workspace(int64_t n, int32_t n_experts, int32_t k);
+int nomad_route(const void* logits, int32_t dtype, int64_t n, int64_t stride, int32_t n_experts, int32_t k, int32_t normalize, int32_t* experts,
+                float* weights, int32_t* offsets, int32_t* order, int32_t* slots, void* workspace, int64_t workspace_bytes, int32_t device, void* stream);
+
+/* dlogits [n, n_experts] of `dtype`, contiguous, from dweights [n, k]: the gradient through the weights (which experts are
+ * chosen has none).  normalize as in the call that made experts and weights. */
+int nomad_route_gradient(const void* logits, int32_t dtype, int64_t n, int64_t stride, int32_t n_experts, int32_t k, int32_t normalize,
+                         const int32_t* experts, const float* weights, const float* dweights, void* dlogits, int32_t device, void* stream);
+
+/*
+ * y_p = act(x_r W_e^T + b_e) for the rows p = offsets[e] .. offsets[e+1] - 1 of every group e, with r = p, or
+ * r = order[p] / per_row where `order` is given; rows of y behind the last group are 0, and so is a row x_r whose r is no
+ * row of x (a negative entry of order).  offsets[0] is 0 and offsets ascend; entries outside 0..rows count as the nearer end.
+ *
+ *   x          [x_rows, in] of `dtype`, columns contiguous; W [n_groups, out, in] of `dtype`, one of its last two strides 1
+ *              (a transposed view gives the gradient of the rows: dx = dy W); bias NULL or [n_groups, out] of `dtype`
+ *   slope_at   NULL, or z [rows, out] of `dtype`: y_p = (x_r W_e^T) act'(z_p) instead, the step back through an activation
+ *              (without bias and z_out)
+ *   y          [rows, out] of out_dtype (`dtype` or NOMAD_F32);  z_out NULL, or [rows, out] of `dtype`: the products with the
+ *              bias, before the activation
+ *
+ * 16-bit operands are multiplied exactly and added up in float32; one rounding per result.
+ */
+typedef struct {
+  uint32_t struct_size; /* = sizeof(nomad_grouped_product_args) */
+  int32_t dtype, out_dtype, activation;
+  int32_t n_groups, per_row;
+  int32_t in, out;
+  int64_t rows, x_rows;
+  const int32_t* offsets;
+  const int32_t* order;
+  const void* x;
+  int64_t x_stride;
+  const void* w;
+  int64_t w_group_stride, w_out_stride, w_in_stride;
+  const void* bias;
+  int64_t bias_stride;
+  const void* slope_at;
+  int64_t slope_stride;
+  void* y;
+  int64_t y_stride;
+  void* z_out;
+  int64_t z_stride;
+  void* stream;
+  int32_t device;
+} nomad_grouped_product_args;
+int nomad_grouped_product(const nomad_grouped_product_args* args);
+
+/*
+ * dW_e = sum of dy_p^T x_r over the rows p of group e (r as above) and db_e = sum of dy_p; groups without rows get zeros.
+ *
+ *   dy [rows, out], x [x_rows, in] of `dtype`;  dw [n_groups, out, in] of out_dtype (`dtype` or NOMAD_F32), contiguous;
+ *   db NULL or [n_groups, out] fp32, contiguous
+ */
+typedef struct {
+  uint32_t struct_size; /* = sizeof(nomad_grouped_gradient_args) */
+  int32_t dtype, out_dtype;
+  int32_t n_groups, per_row;
+  int32_t in, out;
+  int64_t rows, x_rows;
+  const int32_t* offsets;
+  const int32_t* order;
+  const void* dy;
+  int64_t dy_stride;
+  const void* x;
+  int64_t x_stride;
+  void* dw;
+  float* db;
+  void* workspace;
+  int64_t workspace_bytes;
+  void* stream;
+  int32_t device;
+} nomad_grouped_gradient_args;
+int64_t nomad_grouped_gradient_workspace(int64_t rows, int32_t n_groups, int32_t in, int32_t out, int32_t dtype);
+int nomad_grouped_weight_gradient(const nomad_grouped_gradient_args* args);
+
+/*
+ * y_i = sum over j of weights[i, j] values[slots[i, j]] (weights NULL: ones; a slot of -1 adds nothing): the rows' experts
+ * together again.  values [n_values, d] of `dtype`, rows values_stride apart; y [n, d] of `dtype`, contiguous.
+ */
+int nomad_combine(const void* values, int32_t dtype, int64_t n_values, int64_t values_stride, int32_t d, const int32_t* slots, const float* weights,
+                  int64_t n, int32_t k, void* y, int32_t device, void* stream);
+
+/*
+ * Its gradients: dvalues [n_values, d] (NULL: not asked for) gets weights[i, j] dy_i at slots[i, j], and 0 at the places that
+ * `order` (of nomad_route; NULL: no such places) gives no slot; dweights [n, k] fp32 (NULL: not asked for) gets dy_i . values[slots[i, j]], 0
+ * beside a -1.  n_values is n k where order is given.
+ */
+int nomad_combine_gradient(const void* dy, int32_t dtype, int64_t dy_stride, const void* values, int64_t n_values, int64_t values_stride, int32_t d,
+                           const int32_t* slots, const int32_t* order, const float* weights, int64_t n, int32_t k, void* dvalues, float* dweights,
+                           int32_t device, void* stream);
+
+/*
+ * One AdamW step over many tensors:
+ *   m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2;
+ *   p = (1 - lr weight_decay) p - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * with g the gradient times *grad_scale (device memory; NULL: 1).  In place.  p is fp32, bf16 or f16, g of p's type, or fp32, or
+ * (p fp32) any.  bits = 32: m and v fp32 [n].  bits = 8: m int8 [n] and v uint8 [n] codes with a scale (fp32) per block of
+ * NOMAD_ADAMW_BLOCK consecutive elements in m_scale and v_scale: m = s (c / 127) |c / 127|, v = s (c / 255)^4, s the largest
+ * magnitude of the block (0 where that is below 2^-126); c is the whole number with (c - 1/2)^2 <= |m| 127^2 / s < (c + 1/2)^2, to
+ * the fourth power with 255 for v, whose code is at least 1 where v > 0.  A gradient that is NaN or infinite makes its block's
+ * averages NaN.  All zeros is the state before the first step (step = 1).  Tensors and states must not overlap.
+ */
+#define NOMAD_ADAMW_BLOCK 256
+typedef struct {
+  void* p;
+  const void* g;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  int64_t n;
+  int32_t p_dtype, g_dtype;
+} nomad_adamw_tensor;
+typedef struct {
+  uint32_t struct_size; /* = sizeof(nomad_adamw_options) */
+  int32_t bits;
+  int64_t step;
+  double lr, beta1, beta2, eps, weight_decay;
+  const float* grad_scale;
+  void* stream;
+  int32_t device;
+} nomad_adamw_options;
+int nomad_adamw_step(const nomad_adamw_tensor* tensors, int32_t count, const nomad_adamw_options* options);
+
+/* 8-bit states as the fp32 values they stand for: codes[t] (second = 0: int8 of m, 1: uint8 of v) with scales[t], n[t] elements
+ * each, into out[t]; the arrays of addresses are host memory. */
+int nomad_adamw_state_values(const void* const* codes, const float* const* scales, float* const* out, const int64_t* n, int32_t count, int32_t second,
+                             int32_t device, void* stream);
+
 /* Text of the last error of this context ("" if none), or, after a successful nomad_set_graph that had to take a
  * slower path, the reason (see nomad_scatter_path, nomad_edge_pass).  Valid until the next call on it. */
 const char* nomad_last_error(const nomad_ctx* ctx);

@@ -25,7 +25,9 @@ EXPORTS = ["nomad_create", "nomad_destroy", "nomad_set_graph", "nomad_set_embedd
            "nomad_get_embedding", "nomad_get_gradient", "nomad_get_negatives", "nomad_get_means",
            "nomad_get_mean_field", "nomad_num_edges", "nomad_scatter_path", "nomad_edge_pass", "nomad_edges_in_runs", "nomad_device_bytes", "nomad_release_memory", "nomad_tune", "nomad_profile", "nomad_profile_read", "nomad_last_error",
            "nomad_copy_probe", "nomad_gather_probe", "nomad_scatter_probe", "nomad_knn_in_clusters", "nomad_kmeans_lloyd", "nomad_neighbourhood_preservation",
-           "nomad_random_triplet_accuracy", "nomad_random_triplet_accuracy_noalloc", "nomad_pca_init", "nomad_kmeans_lsh_init"]
+           "nomad_random_triplet_accuracy", "nomad_random_triplet_accuracy_noalloc", "nomad_pca_init", "nomad_kmeans_lsh_init",
+           "nomad_route_workspace", "nomad_route", "nomad_route_gradient", "nomad_grouped_product", "nomad_grouped_gradient_workspace",
+           "nomad_grouped_weight_gradient", "nomad_combine", "nomad_combine_gradient", "nomad_adamw_step", "nomad_adamw_state_values"]
 
 
 class NomadConfig(C.Structure):
@@ -42,6 +44,36 @@ EDGES_ROWS, EDGES_RECORDS, EDGES_POOLED, EDGES_EXCHANGED, EDGES_LDS_SUMS = 1, 2,
 PATH_NAMES = {0: "none", 1: "atomic_fp32", 2: "binned", 3: "binned_pooled", 4: "fixed_point_atomics"}
 TUNE = {"edge_block": 1, "workgroups_per_cu": 2, "scatter_path": 3, "pool_kernel": 4, "record_phases": 5, "record_sort": 6, "flush_rounds": 7, "exchange": 8}
 POOL_PICKS16, POOL_DISTINCT, POOL_STRATIFIED = 0, 1, 2
+
+
+class GroupedProductArgs(C.Structure):
+    """nomad_grouped_product_args"""
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("out_dtype", C.c_int32), ("activation", C.c_int32), ("n_groups", C.c_int32),
+                ("per_row", C.c_int32), ("in_", C.c_int32), ("out", C.c_int32), ("rows", C.c_int64), ("x_rows", C.c_int64), ("offsets", C.c_void_p),
+                ("order", C.c_void_p), ("x", C.c_void_p), ("x_stride", C.c_int64), ("w", C.c_void_p), ("w_group_stride", C.c_int64),
+                ("w_out_stride", C.c_int64), ("w_in_stride", C.c_int64), ("bias", C.c_void_p), ("bias_stride", C.c_int64), ("slope_at", C.c_void_p),
+                ("slope_stride", C.c_int64), ("y", C.c_void_p), ("y_stride", C.c_int64), ("z_out", C.c_void_p), ("z_stride", C.c_int64),
+                ("stream", C.c_void_p), ("device", C.c_int32)]
+
+
+class GroupedGradientArgs(C.Structure):
+    """nomad_grouped_gradient_args"""
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("out_dtype", C.c_int32), ("n_groups", C.c_int32), ("per_row", C.c_int32),
+                ("in_", C.c_int32), ("out", C.c_int32), ("rows", C.c_int64), ("x_rows", C.c_int64), ("offsets", C.c_void_p), ("order", C.c_void_p),
+                ("dy", C.c_void_p), ("dy_stride", C.c_int64), ("x", C.c_void_p), ("x_stride", C.c_int64), ("dw", C.c_void_p), ("db", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64), ("stream", C.c_void_p), ("device", C.c_int32)]
+
+
+class AdamWTensor(C.Structure):
+    """nomad_adamw_tensor"""
+    _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("n", C.c_int64), ("p_dtype", C.c_int32), ("g_dtype", C.c_int32)]
+
+
+class AdamWOptions(C.Structure):
+    """nomad_adamw_options"""
+    _fields_ = [("struct_size", C.c_uint32), ("bits", C.c_int32), ("step", C.c_int64), ("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double),
+                ("eps", C.c_double), ("weight_decay", C.c_double), ("grad_scale", C.c_void_p), ("stream", C.c_void_p), ("device", C.c_int32)]
 
 
 class NomadError(RuntimeError):
@@ -99,6 +131,18 @@ def load_library():
     lib.nomad_random_triplet_accuracy_noalloc.argtypes = [vp, i64, i32, vp, i32, i64, C.c_uint64, C.POINTER(i64), i32, vp]
     lib.nomad_pca_init.argtypes = [vp, i64, i32, C.c_float, vp, C.POINTER(C.c_double), C.c_int, i32, vp]
     lib.nomad_kmeans_lsh_init.argtypes = [vp, i64, i32, i32, vp, vp, i32, vp, vp, C.c_int, i32, vp]
+    lib.nomad_route_workspace.argtypes = [i64, i32, i32]
+    lib.nomad_route_workspace.restype = i64
+    lib.nomad_route.argtypes = [vp, i32, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, i64, i32, vp]
+    lib.nomad_route_gradient.argtypes = [vp, i32, i64, i64, i32, i32, i32, vp, vp, vp, vp, i32, vp]
+    lib.nomad_grouped_product.argtypes = [C.POINTER(GroupedProductArgs)]
+    lib.nomad_grouped_gradient_workspace.argtypes = [i64, i32, i32, i32, i32]
+    lib.nomad_grouped_gradient_workspace.restype = i64
+    lib.nomad_grouped_weight_gradient.argtypes = [C.POINTER(GroupedGradientArgs)]
+    lib.nomad_combine.argtypes = [vp, i32, i64, i64, i32, vp, vp, i64, i32, vp, i32, vp]
+    lib.nomad_combine_gradient.argtypes = [vp, i32, i64, vp, i64, i64, i32, vp, vp, vp, i64, i32, vp, vp, i32, vp]
+    lib.nomad_adamw_step.argtypes = [C.POINTER(AdamWTensor), i32, C.POINTER(AdamWOptions)]
+    lib.nomad_adamw_state_values.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp]
     lib.nomad_last_error.argtypes = [vp]
     lib.nomad_last_error.restype = C.c_char_p
     _lib = lib

@@ -1,0 +1,225 @@
+// AdamW over many tensors in one launch (gfx950), states in float32 or in 8 bits.
+//
+//   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  p = (1 - lr wd) p - (lr / c1) m / (sqrt(v) / sqrt(c2) + eps)
+//
+// One pass over the elements, eight neighbouring ones a lane: bound by their bytes (28 an element in float32, 10 with 16-bit
+// parameters and 8-bit states), and with 8-bit states nearly as much by the arithmetic of decoding and encoding.
+//
+// 8 bits: blocks of 256 elements (the 32 lanes of half a wavefront) have one float32 scale s, their largest magnitude.
+// m = s (c / 127) |c / 127| and v = s (c / 255)^4: codes are denser near zero, where most of a block's averages are (v spans
+// 2.4e-10 of its block's largest; a linear code would round the small ones to zero and their steps to m / eps).  A code is the
+// whole number c with (c - 1/2)^2 <= t < (c + 1/2)^2 for t = |m| (127^2 / s), to the fourth power for v with t = v (255^4 / s);
+// v's is 0 only where v is.  The averages round every operation once, without fused ones, and borders are compared in float32: the
+// codes are the same whatever computes them.  The step itself uses the hardware's reciprocal and root (one unit in the last place each).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace nomad_adamw {
+
+constexpr int kTensors = 64;              // a launch: their addresses are its arguments (under 4 KB)
+constexpr int kThreads = 256, kPer = 8;   // lanes a workgroup, elements a lane
+constexpr int kChunk = kThreads * kPer;   // elements a workgroup
+constexpr int kBlock = 256;               // elements a scale
+constexpr int kLanes = kBlock / kPer;
+
+struct Tensor {
+    void* p;
+    const void* g;
+    void* m;
+    void* v;
+    float* m_scale;
+    float* v_scale;
+    int64_t n;
+};
+struct Scalars {
+    float keep, rate, b1, c1, b2, c2, root, eps;
+    const float* grad_scale;   // NULL: 1
+};
+struct Batch {
+    Tensor t[kTensors];
+    uint32_t first[kTensors + 1];   // workgroup of each tensor
+    int32_t count;
+    Scalars s;
+};
+
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void load8(const T* from, int n, T (&v)[kPer]) {
+    struct alignas(sizeof(T) * 4 < 16 ? sizeof(T) * kPer : 16) Part { T v[kPer]; };
+    if (WHOLE) {
+        *(Part*)v = *(const Part*)from;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) v[i] = i < n ? from[i] : (T)0;
+    }
+}
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void store8(T* to, int n, const T (&v)[kPer]) {
+    struct alignas(sizeof(T) * 4 < 16 ? sizeof(T) * kPer : 16) Part { T v[kPer]; };
+    if (WHOLE) {
+        *(Part*)to = *(const Part*)v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (i < n) to[i] = v[i];
+    }
+}
+
+__device__ __forceinline__ float decode_first(int c, float s) {
+#pragma clang fp contract(off)
+    const float t = (float)c * (1.f / 127.f);
+    return (t * fabsf(t)) * s;
+}
+__device__ __forceinline__ float decode_second(uint32_t c, float s) {
+#pragma clang fp contract(off)
+    float t = (float)c * (1.f / 255.f);
+    t = t * t;
+    return (t * t) * s;
+}
+// largest magnitude of the block's 32 lanes, as bits: a NaN is larger than every number
+__device__ __forceinline__ uint32_t block_most(uint32_t bits) {
+#pragma unroll
+    for (int d = kLanes / 2; d > 0; d >>= 1) {
+        const uint32_t o = (uint32_t)__shfl_xor((int)bits, d);
+        bits = o > bits ? o : bits;
+    }
+    return bits;
+}
+// (a NaN or an infinity makes the scale one, and so the block's values NaN: they do not disappear)
+__device__ __forceinline__ float scale_of(uint32_t bits) {
+    return bits < 0x00800000u ? 0.f : __uint_as_float(bits);
+}
+__device__ __forceinline__ int encode_first(float m, float factor) {
+#pragma clang fp contract(off)
+    const float t = fabsf(m) * factor;
+    float c = rintf(__builtin_amdgcn_sqrtf(t));
+    const float up = c + 0.5f, down = c - 0.5f;
+    c += (t >= up * up ? 1.f : 0.f) - (t < down * down && c > 0.f ? 1.f : 0.f);
+    const int code = c == c ? (int)c : 0;
+    return m < 0.f ? -code : code;
+}
+__device__ __forceinline__ uint32_t encode_second(float v, float factor) {
+#pragma clang fp contract(off)
+    const float t = v * factor;
+    float c = rintf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(t)));
+    float up = c + 0.5f, down = c - 0.5f;
+    up = up * up;
+    down = down * down;
+    c += (t >= up * up ? 1.f : 0.f) - (t < down * down && c > 0.f ? 1.f : 0.f);
+    const uint32_t code = c == c ? (uint32_t)c : 0u;
+    return v > 0.f && factor > 0.f && code == 0 ? 1u : code;
+}
+
+template <typename P, typename G, bool EIGHT, bool WHOLE>
+__device__ __forceinline__ void step8(const Tensor& t, const Scalars& s, int64_t at, int n) {
+#pragma clang fp contract(off)
+    P p[kPer];
+    G g[kPer];
+    float m[kPer], v[kPer];
+    load8<P, WHOLE>((const P*)t.p + at, n, p);
+    load8<G, WHOLE>((const G*)t.g + at, n, g);
+    if (EIGHT) {
+        int8_t mc[kPer];
+        uint8_t vc[kPer];
+        load8<int8_t, WHOLE>((const int8_t*)t.m + at, n, mc);
+        load8<uint8_t, WHOLE>((const uint8_t*)t.v + at, n, vc);
+        float ms = 0.f, vs = 0.f;
+        if (n > 0) { ms = t.m_scale[at / kBlock]; vs = t.v_scale[at / kBlock]; }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) { m[i] = decode_first(mc[i], ms); v[i] = decode_second(vc[i], vs); }
+    } else {
+        load8<float, WHOLE>((const float*)t.m + at, n, m);
+        load8<float, WHOLE>((const float*)t.v + at, n, v);
+    }
+    const float scale = s.grad_scale ? *s.grad_scale : 1.f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const float d = (float)g[i] * scale;
+        m[i] = m[i] * s.b1 + d * s.c1;
+        v[i] = v[i] * s.b2 + (d * d) * s.c2;
+        const float step = (m[i] * s.rate) * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[i]) * s.root + s.eps);
+        p[i] = (P)((float)p[i] * s.keep - step);
+    }
+    store8<P, WHOLE>((P*)t.p + at, n, p);
+    if (EIGHT) {
+        uint32_t m_most = 0, v_most = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const uint32_t mb = i < n ? __float_as_uint(m[i]) & 0x7fffffffu : 0u, vb = i < n ? __float_as_uint(v[i]) & 0x7fffffffu : 0u;
+            m_most = mb > m_most ? mb : m_most;
+            v_most = vb > v_most ? vb : v_most;
+        }
+        const float ms = scale_of(block_most(m_most)), vs = scale_of(block_most(v_most));
+        const float mf = ms == 0.f ? 0.f : 16129.f / ms, vf = vs == 0.f ? 0.f : 4228250625.f / vs;
+        int8_t mc[kPer];
+        uint8_t vc[kPer];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) { mc[i] = (int8_t)encode_first(m[i], mf); vc[i] = (uint8_t)encode_second(v[i], vf); }
+        store8<int8_t, WHOLE>((int8_t*)t.m + at, n, mc);
+        store8<uint8_t, WHOLE>((uint8_t*)t.v + at, n, vc);
+        if (n > 0 && at % kBlock == 0) { t.m_scale[at / kBlock] = ms; t.v_scale[at / kBlock] = vs; }
+    } else {
+        store8<float, WHOLE>((float*)t.m + at, n, m);
+        store8<float, WHOLE>((float*)t.v + at, n, v);
+    }
+}
+
+__device__ __forceinline__ bool aligned(const void* p, uintptr_t bytes) { return (uintptr_t)p % bytes == 0; }
+
+template <typename P, typename G, bool EIGHT>
+__global__ void __launch_bounds__(kThreads) k_adamw(Batch b) {
+    int lo = 0, hi = b.count;   // the tensor of this workgroup
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (b.first[mid] <= blockIdx.x) lo = mid;
+        else hi = mid;
+    }
+    const Tensor t = b.t[lo];
+    const int64_t first = (int64_t)(blockIdx.x - b.first[lo]) * kChunk, at = first + (int64_t)threadIdx.x * kPer;
+    const bool whole = first + kChunk <= t.n && aligned(t.p, sizeof(P) * 4 < 16 ? sizeof(P) * kPer : 16) && aligned(t.g, sizeof(G) * 4 < 16 ? sizeof(G) * kPer : 16) &&
+                       aligned(t.m, EIGHT ? 8 : 16) && aligned(t.v, EIGHT ? 8 : 16);
+    if (whole) step8<P, G, EIGHT, true>(t, b.s, at, kPer);
+    else step8<P, G, EIGHT, false>(t, b.s, at, (int)(t.n - at > kPer ? kPer : t.n - at));   // (every lane stays: the block's largest is found by all)
+}
+
+// 8-bit states as the values they stand for
+struct ValuesBatch {
+    struct { const void* codes; const float* scale; float* out; int64_t n; } t[kTensors];
+    uint32_t first[kTensors + 1];
+    int32_t count;
+};
+template <bool SECOND>
+__global__ void __launch_bounds__(kThreads) k_adamw_values(ValuesBatch b) {
+    int lo = 0, hi = b.count;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (b.first[mid] <= blockIdx.x) lo = mid;
+        else hi = mid;
+    }
+    const auto t = b.t[lo];
+    const int64_t first = (int64_t)(blockIdx.x - b.first[lo]) * kChunk;
+#pragma unroll
+    for (int part = 0; part < kPer / 4; ++part) {   // four elements a lane at a time: a wavefront's stores are one run
+        const int64_t at = first + part * (kThreads * 4) + threadIdx.x * 4;
+        if (at >= t.n) return;
+        const float s = t.scale[at / kBlock];
+        const bool whole = at + 4 <= t.n && aligned(t.codes, 4) && aligned(t.out, 16);
+        uint8_t c[4] = {};
+        if (whole) *(uint32_t*)c = *(const uint32_t*)((const uint8_t*)t.codes + at);
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (at + i < t.n) c[i] = ((const uint8_t*)t.codes)[at + i];
+        float4 v;
+        float* x = (float*)&v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = SECOND ? decode_second(c[i], s) : decode_first((int8_t)c[i], s);
+        if (whole) *(float4*)(t.out + at) = v;
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (at + i < t.n) t.out[at + i] = x[i];
+    }
+}
+
+}  // namespace nomad_adamw

@@ -202,6 +202,12 @@ struct HostArrays {   // small host arrays that travel to the device in one copy
         if (e_ != hipSuccess) return e_ == hipErrorOutOfMemory ? NOMAD_E_OOM : NOMAD_E_HIP; \
     } while (0)
 
+// workgroups in two dimensions: one holds fewer than 2^32 lanes
+inline dim3 grid_of(int64_t blocks) {
+    constexpr int64_t row = 1 << 20;
+    return blocks <= row ? dim3((uint32_t)blocks) : dim3((uint32_t)row, (uint32_t)((blocks + row - 1) / row));
+}
+
 inline uint32_t blocks_of(int64_t items, int per) { return (uint32_t)((items + per - 1) / per); }
 
 }  // namespace

@@ -1,0 +1,378 @@
+"""The operators of a learned map: router, products grouped by expert, weighted sum, AdamW (the second half of
+include/nomad.h).
+
+Tensors live on one GPU; a call checks them, takes what it returns from torch's allocator, enqueues the library's kernels on the
+current stream (or `stream`) and returns without waiting.  Gradients are calls of their own: the framework has no
+tape.  Arguments that do not fit raise ValueError before anything is enqueued."""
+from __future__ import annotations
+
+import ctypes as C
+from typing import NamedTuple
+
+from . import binding
+from .binding import NomadError, load_library
+
+MAX_K, MAX_EXPERTS, BLOCK = 8, 16384, 256
+ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3}
+_DTYPES = None
+
+
+def _dtypes():
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    return _DTYPES
+
+
+def _dtype(t, name):
+    code = _dtypes().get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16, not {t.dtype}")
+    return code
+
+
+def _on(device, **tensors):
+    """The tensors that are not None live on `device` (a torch.device of a GPU)."""
+    if device.type != "cuda":
+        raise ValueError("the operators take tensors on the GPU")
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, not on {device}")
+
+
+def _whole(t, name, dtype, shape):
+    """`t` is contiguous, of that type and shape."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+
+
+def _rows(t, name, columns=None):
+    """(rows, stride) of a matrix whose columns are contiguous."""
+    if t.dim() != 2 or (columns is not None and t.shape[1] != columns):
+        raise ValueError(f"{name} must be a matrix" + (f" of {columns} columns" if columns is not None else "") + f", got shape {tuple(t.shape)}")
+    if t.shape[1] > 1 and t.stride(1) != 1 and t.numel():
+        raise ValueError(f"the columns of {name} must be contiguous (strides {t.stride()})")
+    return t.shape[0], (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def _stream(device, stream, used):
+    """The stream of a call.  What it uses of torch's memory is not handed out again before a stream other than the current one
+    has come by here."""
+    import torch
+    chosen = binding._call_stream(device.index, stream)
+    if stream is not None and chosen != torch._C._cuda_getCurrentRawStream(device.index):
+        other = torch.cuda.ExternalStream(int(chosen), device=device)
+        for t in used:
+            if t is not None and t.numel():
+                t.record_stream(other)
+    return int(chosen)
+
+
+def _check(rc, name):
+    if rc:
+        raise NomadError(rc, name)
+
+
+class Routing(NamedTuple):
+    """What `route` returns (include/nomad.h): experts int32 [n, k], weights float32 [n, k], offsets int32 [n_experts + 1],
+    order int32 [n k], slots int32 [n, k]."""
+    experts: object
+    weights: object
+    offsets: object
+    order: object
+    slots: object
+
+
+def route(logits, k, normalize=True, stream=None) -> Routing:
+    """nomad_route: the k experts with the largest logits of every row [n, n_experts], their weights, and the rows in the order
+    of their experts."""
+    import torch
+    device = logits.device
+    _on(device)
+    code = _dtype(logits, "logits")
+    n, stride = _rows(logits, "logits")
+    experts = logits.shape[1]
+    k = int(k)
+    if not 1 <= k <= min(MAX_K, experts) or experts > MAX_EXPERTS:
+        raise ValueError(f"k = {k} of {experts} experts: 1 <= k <= {MAX_K} and no more than there are (at most {MAX_EXPERTS})")
+    lib = load_library()
+    # one allocation: experts, weights, order and slots of n k words each, the offsets, the work space
+    words = n * k
+    need = lib.nomad_route_workspace(n, experts, k)
+    held = torch.empty(4 * words + experts + 1 + need // 4, dtype=torch.int32, device=device)
+    parts = held.split_with_sizes([words, words, words, words, experts + 1, need // 4])
+    out = Routing(parts[0].view(n, k), parts[1].view(torch.float32).view(n, k), parts[4], parts[2], parts[3].view(n, k))
+    st = _stream(device, stream, (logits, held))
+    base = held.data_ptr()
+    _check(lib.nomad_route(logits.data_ptr(), code, n, stride, experts, k, 1 if normalize else 0, base, base + 4 * words, base + 16 * words, base + 8 * words,
+                           base + 12 * words, base + 4 * (4 * words + experts + 1), need, device.index, st or None), "nomad_route")
+    return out
+
+
+def route_gradient(logits, routing, dweights, normalize=True, stream=None):
+    """nomad_route_gradient: the gradient of the logits from that of the weights; normalize as in the call of `route`."""
+    import torch
+    device = logits.device
+    _on(device, experts=routing.experts, weights=routing.weights, dweights=dweights)
+    code = _dtype(logits, "logits")
+    n, stride = _rows(logits, "logits")
+    k = routing.experts.shape[1]
+    _whole(routing.experts, "routing.experts", torch.int32, (n, k))
+    _whole(routing.weights, "routing.weights", torch.float32, (n, k))
+    _whole(dweights, "dweights", torch.float32, (n, k))
+    out = torch.empty(n, logits.shape[1], dtype=logits.dtype, device=device)
+    st = _stream(device, stream, (logits, routing.experts, routing.weights, dweights, out))
+    _check(load_library().nomad_route_gradient(logits.data_ptr(), code, n, stride, logits.shape[1], k, 1 if normalize else 0, routing.experts.data_ptr(),
+                                               routing.weights.data_ptr(), dweights.data_ptr(), out.data_ptr(), device.index, st or None), "nomad_route_gradient")
+    return out
+
+
+def _grouping(x, offsets, order, per_row, rows):
+    """Checks of what says which row of x stands at which place; the number of places."""
+    import torch
+    if offsets.dtype != torch.int32 or offsets.dim() != 1 or not offsets.is_contiguous() or offsets.numel() < 2:
+        raise ValueError("offsets must be a contiguous int32 tensor of one entry more than there are groups")
+    if order is not None:
+        if order.dtype != torch.int32 or order.dim() != 1 or not order.is_contiguous():
+            raise ValueError("order must be a contiguous int32 tensor")
+        if int(per_row) < 1:
+            raise ValueError("per_row must be at least 1")
+        places = order.numel()
+        if places and not x.shape[0]:
+            raise ValueError("order asks for rows of an empty x")
+    else:
+        places = x.shape[0]
+    if rows is not None and rows != places:
+        raise ValueError(f"{places} places, but {rows} rows")
+    return places
+
+
+def grouped_product(x, w, offsets, bias=None, activation=None, order=None, per_row=1, keep=False, slope_at=None, out_dtype=None, stream=None):
+    """nomad_grouped_product: y_p = act(x_p W_e^T + b_e) for the places p of every group e (offsets [E + 1]), x_p = x[p] or
+    x[order[p] // per_row].  w [E, out, in] in either order of its last two strides; keep=True returns (y, z) with z the products
+    before the activation; slope_at=z multiplies by the activation's slope at z instead (the way back)."""
+    import torch
+    device = x.device
+    _on(device, w=w, offsets=offsets, bias=bias, order=order, slope_at=slope_at)
+    code = _dtype(x, "x")
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(k for k in ACTIVATIONS if k)}")
+    if w.dim() != 3 or w.dtype != x.dtype or x.dim() != 2 or w.shape[2] != x.shape[1] or min(w.shape) < 1:
+        raise ValueError(f"w must be [experts, out, {x.shape[-1]}] of {x.dtype}, got {tuple(w.shape)} of {w.dtype}")
+    groups, out, inner = w.shape
+    x_rows, x_stride = _rows(x, "x")
+    places = _grouping(x, offsets, order, per_row, None)
+    if offsets.numel() != groups + 1:
+        raise ValueError(f"{groups} groups need {groups + 1} offsets, got {offsets.numel()}")
+    sg, so, si = w.stride()
+    if inner == 1:
+        si = 1
+    if out == 1 and si != 1:
+        so = 1
+    if si != 1 and so != 1:
+        raise ValueError(f"one of the last two strides of w must be 1 (strides {w.stride()}): .contiguous() copies it")
+    if bias is not None:
+        if bias.dtype != x.dtype or tuple(bias.shape) != (groups, out) or (out > 1 and bias.stride(1) != 1):
+            raise ValueError(f"bias must be [{groups}, {out}] of {x.dtype} with contiguous rows")
+    z_stride = 0
+    if slope_at is not None:
+        if bias is not None or keep:
+            raise ValueError("slope_at goes without bias and keep")
+        if slope_at.dtype != x.dtype or slope_at.shape[0] != places:
+            raise ValueError(f"slope_at must be [{places}, {out}] of {x.dtype}")
+        _, z_stride = _rows(slope_at, "slope_at", out)
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    if out_dtype not in (x.dtype, torch.float32):
+        raise ValueError("out_dtype must be x's type or float32")
+    y = torch.empty(places, out, dtype=out_dtype, device=device)
+    z = torch.empty(places, out, dtype=x.dtype, device=device) if keep else None
+    st = _stream(device, stream, (x, w, offsets, bias, order, slope_at, y, z))
+    a = binding.GroupedProductArgs(
+        C.sizeof(binding.GroupedProductArgs), code, _dtypes()[out_dtype], ACTIVATIONS[activation], groups, int(per_row), inner, out, places, x_rows,
+        offsets.data_ptr(), order.data_ptr() if order is not None else None, x.data_ptr(), x_stride, w.data_ptr(), sg if groups > 1 else 0, so, si,
+        bias.data_ptr() if bias is not None else None, (bias.stride(0) if groups > 1 else 0) if bias is not None else 0,
+        slope_at.data_ptr() if slope_at is not None else None, z_stride, y.data_ptr(), out, z.data_ptr() if keep else None, out, st or None, device.index)
+    _check(load_library().nomad_grouped_product(C.byref(a)), "nomad_grouped_product")
+    return (y, z) if keep else y
+
+
+def grouped_weight_gradient(dy, x, offsets, order=None, per_row=1, bias=True, out_dtype=None, stream=None):
+    """nomad_grouped_weight_gradient: (dW [E, out, in], db [E, out] float32 or None) from dy [places, out] and the x, offsets and
+    order of the product."""
+    import torch
+    device = x.device
+    _on(device, dy=dy, offsets=offsets, order=order)
+    code = _dtype(x, "x")
+    if dy.dtype != x.dtype:
+        raise ValueError(f"dy is {dy.dtype}, x {x.dtype}")
+    x_rows, x_stride = _rows(x, "x")
+    rows, dy_stride = _rows(dy, "dy")
+    _grouping(x, offsets, order, per_row, rows)
+    groups, inner, out = offsets.numel() - 1, x.shape[1], dy.shape[1]
+    if inner < 1 or out < 1:
+        raise ValueError("x and dy need columns")
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    if out_dtype not in (x.dtype, torch.float32):
+        raise ValueError("out_dtype must be x's type or float32")
+    lib = load_library()
+    dw = torch.empty(groups, out, inner, dtype=out_dtype, device=device)
+    db = torch.empty(groups, out, dtype=torch.float32, device=device) if bias else None
+    need = lib.nomad_grouped_gradient_workspace(rows, groups, inner, out, code)
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    st = _stream(device, stream, (x, dy, offsets, order, dw, db, work))
+    a = binding.GroupedGradientArgs(
+        C.sizeof(binding.GroupedGradientArgs), code, _dtypes()[out_dtype], groups, int(per_row), inner, out, rows, x_rows, offsets.data_ptr(),
+        order.data_ptr() if order is not None else None, dy.data_ptr(), dy_stride, x.data_ptr(), x_stride, dw.data_ptr(), db.data_ptr() if bias else None,
+        work.data_ptr() if need else None, need, st or None, device.index)
+    _check(lib.nomad_grouped_weight_gradient(C.byref(a)), "nomad_grouped_weight_gradient")
+    return dw, db
+
+
+def combine(values, slots, weights=None, stream=None):
+    """nomad_combine: y_i = sum_j weights[i, j] values[slots[i, j]] (weights None: ones)."""
+    import torch
+    device = values.device
+    _on(device, slots=slots, weights=weights)
+    code = _dtype(values, "values")
+    n_values, stride = _rows(values, "values")
+    n, k = slots.shape
+    _whole(slots, "slots", torch.int32, (n, k))
+    if weights is not None:
+        _whole(weights, "weights", torch.float32, (n, k))
+    y = torch.empty(n, values.shape[1], dtype=values.dtype, device=device)
+    st = _stream(device, stream, (values, slots, weights, y))
+    _check(load_library().nomad_combine(values.data_ptr(), code, n_values, stride, values.shape[1], slots.data_ptr(),
+                                        weights.data_ptr() if weights is not None else None, n, k, y.data_ptr(), device.index, st or None), "nomad_combine")
+    return y
+
+
+def combine_gradient(dy, values, slots, weights=None, order=None, need_dvalues=True, need_dweights=True, stream=None):
+    """nomad_combine_gradient: (dvalues like values, dweights [n, k] float32); what is not needed is None.  With `order` (of
+    `route`) the places that no slot takes get zeros; without it every place must be some slot's."""
+    import torch
+    device = values.device
+    _on(device, dy=dy, slots=slots, weights=weights, order=order)
+    code = _dtype(values, "values")
+    n_values, stride = _rows(values, "values")
+    d = values.shape[1]
+    n, k = slots.shape
+    _whole(slots, "slots", torch.int32, (n, k))
+    if weights is not None:
+        _whole(weights, "weights", torch.float32, (n, k))
+    if order is not None:
+        _whole(order, "order", torch.int32, (n * k,))
+        if n_values != n * k:
+            raise ValueError(f"order says {n * k} places, values has {n_values}")
+    if dy.dtype != values.dtype or dy.shape[0] != n:
+        raise ValueError(f"dy must be [{n}, {d}] of {values.dtype}")
+    _, dy_stride = _rows(dy, "dy", d)
+    if not need_dvalues and not need_dweights:
+        raise ValueError("neither gradient is asked for")
+    dvalues = torch.empty(n_values, d, dtype=values.dtype, device=device) if need_dvalues else None
+    dweights = torch.empty(n, k, dtype=torch.float32, device=device) if need_dweights else None
+    st = _stream(device, stream, (dy, values, slots, weights, order, dvalues, dweights))
+    _check(load_library().nomad_combine_gradient(
+        dy.data_ptr(), code, dy_stride, values.data_ptr(), n_values, stride, d, slots.data_ptr(), order.data_ptr() if order is not None else None,
+        weights.data_ptr() if weights is not None else None, n, k, dvalues.data_ptr() if need_dvalues else None,
+        dweights.data_ptr() if need_dweights else None, device.index, st or None), "nomad_combine_gradient")
+    return dvalues, dweights
+
+
+class State8(NamedTuple):
+    """An average in 8 bits: codes (int8 of the first, uint8 of the second) [n] and the scales float32 of blocks of 256."""
+    codes: object
+    scales: object
+
+
+def adamw_state(param, bits=32):
+    """(first, second) averages of a tensor before its first step: float32 tensors, or State8 with bits=8."""
+    import torch
+    if bits == 32:
+        return torch.zeros(param.shape, dtype=torch.float32, device=param.device), torch.zeros(param.shape, dtype=torch.float32, device=param.device)
+    if bits != 8:
+        raise ValueError("bits must be 8 or 32")
+    n = param.numel()
+    blocks = -(-n // BLOCK)
+    return tuple(State8(torch.zeros(n, dtype=d, device=param.device), torch.zeros(blocks, dtype=torch.float32, device=param.device)) for d in (torch.int8, torch.uint8))
+
+
+def adamw_step(params, grads, first, second, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_scale=None, stream=None):
+    """nomad_adamw_step: one step, in place, over all of the tensors at once.  first and second: the averages of `adamw_state`
+    (all in 32 bits, or all in 8); step counts from 1; grad_scale: None or a float32 tensor of one element on the GPU."""
+    import torch
+    params, grads, first, second = list(params), list(grads), list(first), list(second)
+    if not len(params) == len(grads) == len(first) == len(second):
+        raise ValueError("params, grads, first and second must be lists of the same length")
+    if not params:
+        return
+    eight = not isinstance(first[0], torch.Tensor)
+    device = params[0].device
+    _on(device, grad_scale=grad_scale)
+    if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
+        raise ValueError("grad_scale must be one float32 element")
+    codes = _dtypes()
+    table = (binding.AdamWTensor * len(params))()
+    used = [grad_scale]
+    for row, p, g, m, v in zip(table, params, grads, first, second):
+        n = p.numel()
+        if p.dtype not in codes or (g.dtype != p.dtype and g.dtype != torch.float32 and (p.dtype != torch.float32 or g.dtype not in codes)):
+            raise ValueError(f"no step for {p.dtype} with gradients in {g.dtype}")
+        if isinstance(m, torch.Tensor) == eight or isinstance(v, torch.Tensor) == eight:
+            raise ValueError("the states must all be in 32 bits, or all in 8")
+        if eight:
+            (m, ms), (v, vs) = m, v
+            blocks = -(-n // BLOCK)
+            if m.dtype != torch.int8 or v.dtype != torch.uint8 or ms.dtype != torch.float32 or vs.dtype != torch.float32 or ms.numel() != blocks or vs.numel() != blocks:
+                raise ValueError(f"8-bit states of {n} elements: int8 and uint8 codes and {blocks} float32 scales each")
+            more = (ms, vs)
+            row.m_scale, row.v_scale = ms.data_ptr(), vs.data_ptr()
+        else:
+            if m.dtype != torch.float32 or v.dtype != torch.float32:
+                raise ValueError("32-bit states are float32")
+            more = ()
+        if g.numel() != n or m.numel() != n or v.numel() != n:
+            raise ValueError("a tensor, its gradient and its states must have as many elements")
+        for t in (p, g, m, v) + more:
+            if t.device != device or not t.is_contiguous():
+                raise ValueError(f"tensors must be contiguous and on {device}")
+        row.p, row.g, row.m, row.v, row.n, row.p_dtype, row.g_dtype = p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), n, codes[p.dtype], codes[g.dtype]
+        if stream is not None:
+            used.extend((p, g, m, v) + more)
+    st = _stream(device, stream, used)
+    options = binding.AdamWOptions(C.sizeof(binding.AdamWOptions), 8 if eight else 32, int(step), float(lr), float(betas[0]), float(betas[1]), float(eps),
+                                   float(weight_decay), grad_scale.data_ptr() if grad_scale is not None else None, st or None, device.index)
+    _check(load_library().nomad_adamw_step(table, len(params), C.byref(options)), "nomad_adamw_step")
+
+
+def adamw_state_values(states, stream=None):
+    """nomad_adamw_state_values: 8-bit averages (a list of State8, all first or all second ones) as float32 tensors."""
+    import torch
+    states = [State8(*s) for s in states]
+    if not states:
+        return []
+    device, dtype = states[0].codes.device, states[0].codes.dtype
+    _on(device)
+    if dtype not in (torch.int8, torch.uint8):
+        raise ValueError("codes are int8 (first averages) or uint8 (second)")
+    for s in states:
+        n = s.codes.numel()
+        _on(device, codes=s.codes, scales=s.scales)
+        if s.codes.dtype != dtype or not s.codes.is_contiguous():
+            raise ValueError("codes must be contiguous, and all first or all second averages")
+        _whole(s.scales, "scales", torch.float32, (-(-n // BLOCK),))
+    sizes = [s.codes.numel() for s in states]
+    # one allocation; every tensor begins on a border of 16 bytes
+    starts, total = [], 0
+    for n in sizes:
+        starts.append(total)
+        total += -(-n // 4) * 4
+    held = torch.empty(total, dtype=torch.float32, device=device)
+    out = [held[at:at + n] for at, n in zip(starts, sizes)]
+    count = len(states)
+    addresses, words = C.c_void_p * count, C.c_int64 * count
+    st = _stream(device, stream, [held] + [t for s in states for t in s])
+    _check(load_library().nomad_adamw_state_values(addresses(*[s.codes.data_ptr() for s in states]), addresses(*[s.scales.data_ptr() for s in states]),
+                                                   addresses(*[t.data_ptr() for t in out]), words(*sizes), count, 1 if dtype == torch.uint8 else 0, device.index,
+                                                   st or None), "nomad_adamw_state_values")
+    return out

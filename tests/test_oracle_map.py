@@ -1,0 +1,79 @@
+"""The learned map's oracle against differences and cases worked by hand (no GPU)."""
+import numpy as np
+import pytest
+
+from oracle import map_oracle as mo
+
+
+def _difference(f, x, h=1e-6):
+    g = np.zeros_like(x)
+    for at in np.ndindex(x.shape):
+        up, down = x.copy(), x.copy()
+        up[at] += h
+        down[at] -= h
+        g[at] = (f(up) - f(down)) / (2 * h)
+    return g
+
+
+def test_routing_by_hand():
+    inf = float("inf")
+    logits = np.array([[1.0, 3.0, 3.0, 0.0], [-inf, -inf, -inf, -inf], [float("nan"), 2.0, -inf, 2.0], [0.0, -0.0, -1.0, -inf]])
+    experts, weights, offsets, order, slots = mo.route(logits, 2)
+    assert experts.tolist() == [[1, 2], [-1, -1], [1, 3], [0, 1]]
+    assert np.allclose(weights, [[0.5, 0.5], [0, 0], [0.5, 0.5], [0.5, 0.5]])
+    assert offsets.tolist() == [0, 1, 4, 5, 6]
+    assert order.tolist() == [6, 0, 4, 7, 1, 5, -1, -1]
+    assert slots.tolist() == [[1, 4], [-1, -1], [2, 5], [0, 3]]
+    _, full, _, _, _ = mo.route(logits, 1, normalize=False)
+    e = np.exp([1.0, 3.0, 3.0, 0.0])
+    assert np.isclose(full[0, 0], e[1] / e.sum()) and np.isclose(full[2, 0], 0.5)
+
+
+@pytest.mark.parametrize("normalize", [True, False])
+def test_route_gradient_against_differences(normalize):
+    rng = np.random.default_rng(3)
+    logits, c = rng.normal(size=(5, 7)), rng.normal(size=(5, 3))
+    experts, weights, *_ = mo.route(logits, 3, normalize)
+    got = mo.route_gradient(logits, experts, weights, c, normalize)
+    want = _difference(lambda l: float((mo.route(l, 3, normalize)[1] * c).sum()), logits)
+    assert np.abs(got - want).max() < 1e-8
+
+
+@pytest.mark.parametrize("name", ["none", "relu", "silu", "gelu"])
+def test_slopes_against_differences(name):
+    z = np.array([-6.0, -1.3, -0.2, 0.3, 1.7, 8.0])
+    want = (mo.act(z + 1e-6, name) - mo.act(z - 1e-6, name)) / 2e-6
+    assert np.abs(mo.slope(z, name) - want).max() < 1e-8
+
+
+def test_layer_gradients_against_differences():
+    rng = np.random.default_rng(4)
+    n, k, groups, d, h, o = 6, 2, 3, 4, 5, 2
+    logits = rng.normal(size=(n, groups))
+    logits[2] = -np.inf                                        # a row without experts
+    experts, weights, offsets, order, slots = mo.route(logits, k)
+    x, w1, b1 = rng.normal(size=(n, d)), rng.normal(size=(groups, h, d)), rng.normal(size=(groups, h))
+    w2, c = rng.normal(size=(groups, o, h)), rng.normal(size=(n, o))
+
+    def loss(x, w1, b1, w2):
+        hid, _, _ = mo.product(x, w1, offsets, b1, "silu", order, k)
+        return float((mo.combine(mo.product(hid, w2, offsets)[0], slots, weights) * c).sum())
+    hid, z, _ = mo.product(x, w1, offsets, b1, "silu", order, k)
+    out = mo.product(hid, w2, offsets)[0]
+    do, dweights = mo.combine_gradient(c, out, slots, weights)
+    dw2, _, _, _ = mo.weight_gradient(do, hid, offsets)
+    dz = mo.product(do, w2.transpose(0, 2, 1), offsets, None, "silu", slope_at=z)[0]
+    dw1, db1, _, _ = mo.weight_gradient(dz, x, offsets, order, k)
+    dx = mo.combine(mo.product(dz, w1.transpose(0, 2, 1), offsets)[0], slots)
+    for got, at, f in ((dx, x, lambda v: loss(v, w1, b1, w2)), (dw1, w1, lambda v: loss(x, v, b1, w2)), (db1, b1, lambda v: loss(x, w1, v, w2)),
+                       (dw2, w2, lambda v: loss(x, w1, b1, v))):
+        assert np.abs(got - _difference(f, at)).max() < 1e-7
+    dl = _difference(lambda l: float((mo.combine(out, slots, mo.route(l, k)[1]) * c).sum()), np.where(np.isinf(logits), 0.0, logits))
+    got = mo.route_gradient(logits, experts, weights, dweights)
+    assert np.abs(got - dl)[[0, 1, 3, 4, 5]].max() < 1e-7 and (got[2] == 0).all()
+
+
+def test_adamw_first_step_is_the_sign():
+    p, m, v = mo.adamw(np.array([1.0, -2.0]), np.array([0.5, -3.0]), np.zeros(2), np.zeros(2), 1, 0.1, 0.9, 0.999, 0.0, 0.0)
+    assert np.allclose(p, [0.9, -1.9]) and np.allclose(m, [0.05, -0.3]) and np.allclose(v, [2.5e-4, 9e-3])
+    assert np.allclose(mo.adamw(np.array([1.0]), np.zeros(1), np.zeros(1), np.zeros(1), 1, 0.1, 0.9, 0.999, 1e-8, 0.5)[0], 0.95)
