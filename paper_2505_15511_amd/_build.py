@@ -9,7 +9,8 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
 LIB_PATH = os.environ.get("NOMAD_LIBRARY_PATH") or os.path.join(_PKG, "libnomad.so")
 SOURCES = [os.path.join(_PKG, "csrc", "nomad.hip"), os.path.join(_PKG, "csrc", "knn.hip"), os.path.join(_PKG, "csrc", "knn_filter.hip"),
-           os.path.join(_PKG, "csrc", "pca.hip"), os.path.join(_PKG, "csrc", "probes.hip"), os.path.join(_PKG, "csrc", "grouped.hip"),
+           os.path.join(_PKG, "csrc", "pca.hip"), os.path.join(_PKG, "csrc", "probes.hip"), os.path.join(_PKG, "csrc", "grouped.hip"), os.path.join(_PKG, "csrc", "grouped_bf16.hip"),
+           os.path.join(_PKG, "csrc", "grouped_f16.hip"), os.path.join(_PKG, "csrc", "grouped_f32.hip"),
            os.path.join(_PKG, "csrc", "route.hip"), os.path.join(_PKG, "csrc", "adamw.hip")]
 HEADERS = [os.path.join(_PKG, "csrc", "nomad_kernels.h"), os.path.join(_PKG, "csrc", "knn_kernels.h"),
            os.path.join(_PKG, "csrc", "knn_filter.h"), os.path.join(_PKG, "csrc", "knn_filter_kernel.h"), os.path.join(_PKG, "csrc", "filter_scale.h"),
@@ -19,7 +20,7 @@ HEADERS = [os.path.join(_PKG, "csrc", "nomad_kernels.h"), os.path.join(_PKG, "cs
            os.path.join(_PKG, "csrc", "pca_kernels.h"), os.path.join(_PKG, "csrc", "host_util.h"),
            os.path.join(_PKG, "csrc", "edge_plan.h"), os.path.join(_PKG, "csrc", "exchange_kernels.h"),
            os.path.join(_PKG, "csrc", "run_kernels.h"), os.path.join(_PKG, "csrc", "field_kernels.h"), os.path.join(_PKG, "csrc", "small_kernels.h"), os.path.join(_PKG, "csrc", "kmeans_plan.h"),
-           os.path.join(_PKG, "csrc", "grouped_kernels.h"), os.path.join(_PKG, "csrc", "route_kernels.h"), os.path.join(_PKG, "csrc", "adamw_kernels.h"),
+           os.path.join(_PKG, "csrc", "grouped_kernels.h"), os.path.join(_PKG, "csrc", "grouped_launch.h"), os.path.join(_PKG, "csrc", "grouped_plan.h"), os.path.join(_PKG, "csrc", "route_kernels.h"), os.path.join(_PKG, "csrc", "adamw_kernels.h"),
            os.path.join(_ROOT, "include", "nomad.h")]
 
 

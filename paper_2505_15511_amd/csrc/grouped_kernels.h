@@ -3,12 +3,17 @@
 //   product           y_p = act(x_row(p) W_e^T + b_e)        for o_e <= p < o_{e+1}
 //   weight gradient   dW_e = sum_p dy_p^T x_row(p),  db_e = sum_p dy_p
 //
-// Both are tiles of C[b][a] = sum_k A[a][k] B[b][k] with a running along the result's contiguous columns: a lane of a 16x16
-// matrix instruction ends up with four neighbouring values of a, one 8- or 16-byte store.  Product: a = columns of W's rows,
-// b = rows p, k = columns of x.  Weight gradient: a = columns of x, b = columns of dy, k = rows p of the group.
+// Both are tiles of C[b][a] = sum_k A[a][k] B[b][k] with a running along the result's contiguous columns.  Product: a = columns
+// of W's rows, b = rows p, k = columns of x.  Weight gradient: a = columns of x, b = columns of dy, k = rows p of the group.
+//
+// A wavefront's share of a tile is made of 16x16 matrix instructions.  Which columns the 16 rows r of an instruction stand for is free: in
+// sets of Q instructions, row r of the set's instruction x is column 4 Q (r / 4) + 4 x + r % 4, so that a lane, which holds four
+// rows r of every instruction, ends up with 4 Q neighbouring columns of one row of the result.  Q makes that 16 bytes.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 namespace nomad_grouped {
 
@@ -52,19 +57,32 @@ template <> struct Elem<float> {
 template <typename T>
 __device__ __forceinline__ float to_f32(T v) { return (float)v; }
 
-__device__ __forceinline__ float activate(float z, int act) {
-    if (act == kRelu) return z < 0.f ? 0.f : z;                       // (a NaN stays one)
-    if (act == kSilu) return z / (1.f + __expf(-z));
-    if (act == kGelu) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+template <int V> struct Constant { static constexpr int value = V; };
+
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }   // (the hardware's reciprocal: one unit in the last place)
+
+// 1 + erf(z / sqrt 2): Abramowitz and Stegun, formula 7.1.26, whose error of 1.5e-7 is that of the sum's rounding
+__device__ __forceinline__ float one_plus_erf(float z) {
+    const float x = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * x);
+    const float tail = ((((1.061405429f * t - 1.453152027f) * t + 1.421413741f) * t - 0.284496736f) * t + 0.254829592f) * t * __expf(-x * x);
+    return z < 0.f ? tail : 2.f - tail;
+}
+
+template <int ACT>
+__device__ __forceinline__ float activate(float z) {
+    if (ACT == kRelu) return z < 0.f ? 0.f : z;                       // (a NaN stays one)
+    if (ACT == kSilu) return z * sigmoid(z);
+    if (ACT == kGelu) return 0.5f * z * one_plus_erf(z);
     return z;
 }
-__device__ __forceinline__ float activation_slope(float z, int act) {
-    if (act == kRelu) return z > 0.f ? 1.f : (z != z ? z : 0.f);
-    if (act == kSilu) {
-        const float s = 1.f / (1.f + __expf(-z));
+template <int ACT>
+__device__ __forceinline__ float activation_slope(float z) {
+    if (ACT == kRelu) return z > 0.f ? 1.f : (z != z ? z : 0.f);
+    if (ACT == kSilu) {
+        const float s = sigmoid(z);
         return s + z * s * (1.f - s);
     }
-    if (act == kGelu) return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * __expf(-0.5f * z * z);
+    if (ACT == kGelu) return 0.5f * one_plus_erf(z) + z * 0.39894228040143268f * __expf(-0.5f * z * z);
     return 1.f;
 }
 
@@ -77,13 +95,19 @@ struct Item {
     int32_t group;        // n_groups: rows of no group
     int32_t index;        // of this item among the group's
     int32_t first;        // items before this group's
-    int32_t total;        // items of all groups
+    int32_t items;        // the group has
 };
 
 __device__ __forceinline__ int64_t group_end(const int32_t* offsets, int32_t e, int32_t n_groups, int64_t rows) {   // (whatever the offsets hold, rows stay in range)
     if (e > n_groups) return rows;
     const int64_t o = offsets[e];
     return o < 0 ? 0 : o > rows ? rows : o;
+}
+
+// a lane's value for all, in scalar registers (__shfl leaves one in every lane)
+__device__ __forceinline__ int32_t of_lane(int32_t v, int who) { return __builtin_amdgcn_readlane(v, who); }
+__device__ __forceinline__ int64_t of_lane(int64_t v, int who) {
+    return (int64_t)((uint64_t)(uint32_t)of_lane((int32_t)(v >> 32), who) << 32 | (uint32_t)of_lane((int32_t)v, who));
 }
 
 __device__ __forceinline__ int32_t wave_inclusive(int32_t v, int lane) {
@@ -101,7 +125,6 @@ __device__ __forceinline__ int32_t group_items(int64_t begin, int64_t end, int32
     return tail ? items : items < least ? least : items;
 }
 
-// Item number `at` of the list (total alone, and group -1, where at is beyond it)
 __device__ __forceinline__ int32_t count_items(const int32_t* offsets, int32_t n_groups, int64_t rows, int32_t step, int32_t least, bool tail, int lane) {
     const int32_t groups = n_groups + (tail ? 1 : 0);
     int32_t total = 0;
@@ -109,10 +132,11 @@ __device__ __forceinline__ int32_t count_items(const int32_t* offsets, int32_t n
         const int32_t e = g0 + lane;
         int32_t items = 0;
         if (e < groups) items = group_items(group_end(offsets, e, n_groups, rows), group_end(offsets, e + 1, n_groups, rows), step, least, e == n_groups);
-        total += __shfl(wave_inclusive(items, lane), 63);
+        total += of_lane(wave_inclusive(items, lane), 63);
     }
     return total;
 }
+// Item number `at` of the list (group -1 where it is beyond it)
 __device__ __forceinline__ Item find_item(const int32_t* offsets, int32_t n_groups, int64_t rows, int32_t step, int32_t least, bool tail, int32_t at, int lane) {
     const int32_t groups = n_groups + (tail ? 1 : 0);
     Item it;
@@ -132,14 +156,15 @@ __device__ __forceinline__ Item find_item(const int32_t* offsets, int32_t n_grou
         if (mask) {
             const int who = __builtin_ctzll(mask);
             it.group = g0 + who;
-            it.begin = __shfl(begin, who);
-            it.end = __shfl(end, who);
+            it.begin = of_lane(begin, who);
+            it.end = of_lane(end, who);
             if (it.end < it.begin) it.end = it.begin;
-            it.first = __shfl(upto - items, who);
+            it.first = of_lane(upto - items, who);
+            it.items = of_lane(items, who);
             it.index = at - it.first;
             break;
         }
-        before = __shfl(upto, 63);
+        before = of_lane(upto, 63);
     }
     return it;
 }
@@ -151,16 +176,23 @@ __device__ const uint4 kZeros[1] = {{0, 0, 0, 0}};   // what a lane reads whose 
 constexpr int kStepBytes = 128;   // of k a stage holds
 constexpr int kTileChunks = kStepBytes / 16;
 
-// LDS holds 16-byte chunks.  KC (k is contiguous in memory): rows of 8 chunks, chunk c of row r at place c ^ ((r >> 1) & 7).
-// Otherwise (the tile's own index is contiguous): k rows of TILE elements; a matrix fragment takes 16 elements of several k rows at
-// once, 32 bytes (64 for float32) each, so those units are spread by k.
-template <typename T, int TILE, bool KC>
+// LDS holds 16-byte chunks.  KC (k is contiguous in memory): rows of 8 chunks.  Otherwise (the tile's own index is contiguous): k rows
+// of TILE elements.  Chunk c of row r stands at place c ^ twist(r), so that the lanes that read together meet different banks
+// (measured: no conflicts).  Q as above for the operand a; the other one's fragments are 16 neighbours, Q = 1.
+constexpr int log2_of(int v) { return v <= 1 ? 0 : 1 + log2_of(v / 2); }
+
+template <typename T, int TILE, bool KC, int Q>
 __device__ __forceinline__ int chunk_twist(int row) {
-    if (KC) return (row >> 1) & 7;
-    constexpr int units = TILE * (int)sizeof(T) / (sizeof(T) == 4 ? 64 : 32);   // of a k row
-    constexpr int mask = units >= 8 ? 7 : units - 1;
-    if (sizeof(T) == 4) return ((row >> 2) & mask) << 2;
-    return (((row & 3) | ((row >> 1) & 4)) & mask) << 1;
+    // lanes read one chunk each of 16 rows: neighbours, or fours of neighbours 4 Q apart
+    if (KC) return ((row >> 1) & 1) | ((row >> log2_of(4 * Q)) & 3) << 1;
+    // lanes read pieces of the same columns in several k rows: rows k .. k + 3 together (16 bits, turned on the way), or the k
+    // of the four lane groups (32 bits).  Bits of the row go to bits of the chunk that the columns leave alone.
+    constexpr int chunks = TILE * (int)sizeof(T) / 16, lq = log2_of(Q);
+    int t;
+    if (sizeof(T) == 4) t = ((row >> 2) & 3) << (lq == 0 ? 2 : 3);                  // 16 neighbours: chunks 0..3; Q = 2: 0, 2, 4, 6
+    else if (Q == 1) t = (row & 3) << 1 | ((row >> 3) & 1) << 3;                    // 16 neighbours: chunks 0 and 1
+    else t = (row & 3) << 2;                                                        // Q = 2: chunks 0..3
+    return t & (chunks - 1);
 }
 
 // Where a tile comes from: rows of `length` elements; row r of the source is base + r * stride, or, gathered,
@@ -171,18 +203,17 @@ struct Source {
     const int32_t* order;  // NULL: rows as they are
     int64_t rows;          // of the source, where gathered
     uint32_t per_row;
-    __device__ __forceinline__ int64_t row_of(int64_t p) const {
-        if (!order) return p;
-        const int32_t slot = order[p];
+    __device__ __forceinline__ int64_t row_at(int32_t slot) const {   // of an entry of the order; -1: none
         if (slot < 0) return -1;
         const int64_t r = per_row == 1 ? (uint32_t)slot : (uint32_t)slot / per_row;
         return r < rows ? r : -1;
     }
+    __device__ __forceinline__ int64_t row_of(int64_t p) const { return order ? row_at(order[p]) : p; }
 };
 
-// TILE rows (KC) or columns (not KC) by one stage of k, for NT threads.  ASYNC: loads go to LDS directly, whole 16-byte chunks;
-// otherwise through registers, element by element where a chunk is cut off.
-template <typename T, int TILE, bool KC, bool ASYNC, int NT>
+// TILE rows (KC) or columns (not KC) by one stage of k, for NT threads.  PICKED: source rows anywhere (KC: a pointer each; otherwise
+// their numbers are read a stage ahead).  ASYNC: loads go to LDS directly, whole 16-byte chunks; otherwise through registers, element by element where a chunk is cut off.
+template <typename T, int TILE, bool KC, bool PICKED, int Q, bool ASYNC, int NT>
 struct Operand {
     static constexpr int kEpc = 16 / (int)sizeof(T);             // elements a chunk
     static constexpr int kBk = kStepBytes / (int)sizeof(T);      // k of a stage
@@ -190,10 +221,12 @@ struct Operand {
     static constexpr int kChunks = TILE * kTileChunks;           // of a stage
     static constexpr int kPer = (kChunks + NT - 1) / NT;         // a thread
     static constexpr bool kWhole = kChunks % NT == 0;
-    const T* row[KC ? kPer : 1];   // KC: the thread's rows (NULL: none)
+    const T* row[KC && PICKED ? kPer : 1];   // KC: the thread's rows (picked: NULL where there is none)
+    int32_t rows;                  // KC, not picked: rows there are from the thread's first on
     Source src;
-    int64_t first;                 // not KC: the source row of k = 0
+    int64_t first;                 // not KC: the place of k = 0
     int32_t across;                // not KC: columns before the tile
+    int32_t place[!KC && PICKED ? kPer : 1];   // not KC, picked: entries of the order for the next stage's rows
     int32_t limit;                 // k there are (KC: of every row)
     int32_t width;                 // not KC: columns there are, from the tile's first
     uint4 held[ASYNC ? 1 : kPer];
@@ -204,35 +237,57 @@ struct Operand {
     __device__ __forceinline__ void open_rows(const Source& s, int64_t first_row, int64_t count, int32_t k_limit, int tid) {
         src = s;
         limit = k_limit;
+        if (!PICKED) {
+            const int r = tid / kCpr;
+            row[0] = (const T*)s.base + (first_row + r) * s.stride;
+            rows = (int32_t)(count < TILE ? count : TILE) - r;
+            return;
+        }
 #pragma unroll
         for (int it = 0; it < kPer; ++it) {
             const int r = (it * NT + tid) / kCpr;
-            row[KC ? it : 0] = nullptr;
+            row[PICKED ? it : 0] = nullptr;
             if (has(it, tid) && r < count) {
                 const int64_t at = s.row_of(first_row + r);
-                if (at >= 0) row[KC ? it : 0] = (const T*)s.base + at * s.stride;
+                if (at >= 0) row[PICKED ? it : 0] = (const T*)s.base + at * s.stride;
             }
         }
     }
-    // not KC: columns from `column` on (`columns` in all), k = source rows first_k ..
-    __device__ __forceinline__ void open_columns(const Source& s, int64_t first_k, int32_t k_limit, int32_t column, int32_t columns) {
+    // not KC: columns from `column` on (`columns` in all), k = source rows (places of the order) first_k ..
+    __device__ __forceinline__ void open_columns(const Source& s, int64_t first_k, int32_t k_limit, int32_t column, int32_t columns, int tid) {
         src = s;
         first = first_k;
         limit = k_limit;
         across = column;
         width = columns - column;
+        if (PICKED) fetch(0, tid);
+        else row[0] = (const T*)s.base + (first_k + tid / kCpr) * s.stride + column;
+    }
+    __device__ __forceinline__ void fetch(int32_t k0, int tid) {
+#pragma unroll
+        for (int it = 0; it < kPer; ++it) {
+            const int32_t k = k0 + (it * NT + tid) / kCpr;
+            place[!KC && PICKED ? it : 0] = k >= limit ? -1 : src.order ? src.order[first + k] : (int32_t)(first + k);
+        }
     }
     __device__ __forceinline__ void chunk(int it, int tid, int32_t k0, const T*& from, int& elements) const {
-        const int l = it * NT + tid, r = l / kCpr, c = (l % kCpr) ^ chunk_twist<T, TILE, KC>(r);
+        const int l = it * NT + tid, r = l / kCpr, c = (l % kCpr) ^ chunk_twist<T, TILE, KC, Q>(r);
         if (KC) {
             const int32_t k = k0 + c * kEpc;
-            from = row[KC ? it : 0] + k;
-            elements = row[KC ? it : 0] ? limit - k : 0;
+            constexpr int apart = NT / kCpr;   // rows between the thread's chunks
+            from = PICKED ? row[PICKED ? it : 0] + k : row[0] + (int64_t)(it * apart) * src.stride + k;
+            elements = (PICKED ? row[PICKED ? it : 0] != nullptr : it * apart < rows) ? limit - k : 0;
         } else {
             const int32_t k = k0 + r;
-            const int64_t at = k < limit ? src.row_of(first + k) : -1;
-            from = (const T*)src.base + at * src.stride + across + c * kEpc;
-            elements = at >= 0 ? width - c * kEpc : 0;
+            int64_t at = 0;
+            if (PICKED) {
+                at = src.row_at(place[!KC && PICKED ? it : 0]);
+                from = (const T*)src.base + at * src.stride + across + c * kEpc;
+            } else {
+                constexpr int apart = NT / kCpr;
+                from = row[0] + (int64_t)(k0 + it * apart) * src.stride + c * kEpc;
+            }
+            elements = k < limit && at >= 0 ? width - c * kEpc : 0;
         }
     }
     // asks for the stage that begins at k0
@@ -261,6 +316,7 @@ struct Operand {
                 held[ASYNC ? 0 : it] = v;
             }
         }
+        if (!KC && PICKED) fetch(k0 + kBk, tid);
     }
     // puts down what was asked for, where the loads did not
     __device__ __forceinline__ void put(uint4* lds, int tid) const {
@@ -269,30 +325,32 @@ struct Operand {
         for (int it = 0; it < kPer; ++it)
             if (has(it, tid)) lds[it * NT + tid] = held[ASYNC ? 0 : it];
     }
-    // fragment of the 16 rows (columns) from `at` on, matrix step s of the stage's two
-    static __device__ __forceinline__ uint4 fragment(const uint4* lds, int at, int s, int lane) {
+    // fragment number x of the rows (columns) from `at` on, matrix step s of the stage's two
+    static __device__ __forceinline__ uint4 fragment(const uint4* lds, int at, int x, int s, int lane) {
         const int g = lane >> 4, i = lane & 15;
+        const int set = at + 16 * Q * (x / Q) + 4 * (x % Q), four = set + 4 * Q * (i >> 2);   // the first of lane i's four neighbours
         if (KC) {
-            const int r = at + i;
-            return lds[r * kTileChunks + ((s * 4 + g) ^ chunk_twist<T, TILE, KC>(r))];
+            const int r = four + (i & 3);
+            return lds[r * kTileChunks + ((s * 4 + g) ^ chunk_twist<T, TILE, KC, Q>(r))];
         }
         if (sizeof(T) == 4) {
             uint4 v;
             uint32_t* out = (uint32_t*)&v;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                const int k = s * 16 + 4 * g + t, e = at + i;
-                out[t] = ((const uint32_t*)lds)[(k * kCpr + ((e >> 2) ^ chunk_twist<T, TILE, KC>(k))) * 4 + (e & 3)];
+                const int k = s * 16 + 4 * g + t;
+                out[t] = ((const uint32_t*)lds)[(k * kCpr + ((four >> 2) ^ chunk_twist<T, TILE, KC, Q>(k))) * 4 + (i & 3)];
             }
             return v;
         }
-        // four k rows of 16 elements, turned on the way: lane i of the group gets element i of the four rows
+        // a lane group asks for 16 elements of four k rows, four a lane; they come turned: lane i has element i of the four rows
+        const int part = set + 4 * Q * (i & 3);
         union { i16x4 half[2]; uint4 whole; } v;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int k = s * 32 + 8 * g + 4 * h + (i >> 2), e = at + 4 * (i & 3);
-            const int c = (e >> 3) ^ chunk_twist<T, TILE, KC>(k);
-            v.half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)((const char*)(lds + k * kCpr + c) + (e & 4) * 2));
+            const int k = s * 32 + 8 * g + 4 * h + (i >> 2);
+            const int c = (part >> 3) ^ chunk_twist<T, TILE, KC, Q>(k);
+            v.half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)((const char*)(lds + k * kCpr + c) + (part & 4) * 2));
         }
         return v.whole;
     }
@@ -300,68 +358,90 @@ struct Operand {
 
 // ---- a tile of the result
 
-template <typename T, int TA, int TB, int WA, int WB, bool A_KC, bool B_KC, bool ASYNC>
+template <typename T, typename O, int TA, int TB, int WA, int WB, bool A_KC, bool A_PICKED, bool B_KC, bool B_PICKED, bool ASYNC>
 struct Tile {
     static constexpr int kNt = 64 * WA * WB;
     static constexpr int kFa = TA / WA / 16, kFb = TB / WB / 16;
+    static constexpr int kQ = sizeof(O) == 2 && kFa % 2 == 0 ? 2 : 1, kN = 4 * kQ, kSets = kFa / kQ;   // columns a lane holds side by side, and how often
     static constexpr int kBk = kStepBytes / (int)sizeof(T);
-    typedef Operand<T, TA, A_KC, ASYNC, kNt> A;
-    typedef Operand<T, TB, B_KC, ASYNC, kNt> B;
+    typedef Operand<T, TA, A_KC, A_PICKED, kQ, ASYNC, kNt> A;
+    typedef Operand<T, TB, B_KC, B_PICKED, 1, ASYNC, kNt> B;
     f32x4 acc[kFa][kFb];
 
-    // acc = sum over k < limit; with SUMS also the sums of B alone over k
-    template <bool SUMS>
-    __device__ __forceinline__ void run(A& a, B& b, uint4* a0, uint4* b0, uint4* a1, uint4* b1, int32_t limit, f32x4* sums, int tid) {
-        const int lane = tid & 63, wave = tid >> 6, wa = (wave % WA) * (TA / WA), wb = (wave / WA) * (TB / WB);
+    static __device__ __forceinline__ int column(int set, int tid) { return ((tid >> 6) % WA) * (TA / WA) + 16 * kQ * set + kN * ((tid & 63) >> 4); }   // of the tile: the lane's first
+    static __device__ __forceinline__ int row(int y, int tid) { return ((tid >> 6) / WA) * (TB / WB) + 16 * y + (tid & 15); }
+    __device__ __forceinline__ auto& at(int set, int y, int j) { return ((float*)&acc[set * kQ + j / 4][y])[j % 4]; }
+    __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int x = 0; x < kFa; ++x)
 #pragma unroll
             for (int y = 0; y < kFb; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // 16 rows of the widest result a wavefront, in the stages that the next tile's first loads do not use
+    static constexpr int kPatch = 16 * 16 * kFa * 4, kInA = TA * kStepBytes / kPatch;
+    static_assert(kInA + TB * kStepBytes / kPatch >= WA * WB, "every wavefront has a patch");
+    static __device__ __forceinline__ char* patch(uint4* a1, uint4* b1, int tid) {
+        const int wave = tid >> 6;
+        return wave < kInA ? (char*)a1 + wave * kPatch : (char*)b1 + (wave - kInA) * kPatch;
+    }
+    // every wavefront's loads have landed, then all have arrived (a barrier alone does not wait for loads to LDS)
+    static __device__ __forceinline__ void meet() {
+        if (ASYNC) __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+        __syncthreads();
+    }
+    // acc += sum over k < limit, the first stage having been asked for.  Behind it all four stages are free.  SUMS, where with_sums:
+    // also the sums of B alone over k; the wavefronts side by side along a share their columns, kSums fragments each.
+    static constexpr int kSums = kFb < WA ? 1 : kFb / WA;
+    static __device__ __forceinline__ bool sums_of(int y, int tid) { return y / kSums == (tid >> 6) % WA; }
+    template <bool SUMS>
+    __device__ __forceinline__ void run(A& a, B& b, uint4* a0, uint4* b0, uint4* a1, uint4* b1, int32_t limit, f32x4* sums, bool with_sums, int tid) {
+        const int lane = tid & 63, wave = tid >> 6, wa = (wave % WA) * (TA / WA), wb = (wave / WA) * (TB / WB);
         const auto step = [&](const uint4* la, const uint4* lb) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 uint4 fa[kFa], fb[kFb];
 #pragma unroll
-                for (int x = 0; x < kFa; ++x) fa[x] = A::fragment(la, wa + 16 * x, s, lane);
+                for (int x = 0; x < kFa; ++x) fa[x] = A::fragment(la, wa, x, s, lane);
 #pragma unroll
-                for (int y = 0; y < kFb; ++y) fb[y] = B::fragment(lb, wb + 16 * y, s, lane);
+                for (int y = 0; y < kFb; ++y) fb[y] = B::fragment(lb, wb, y, s, lane);
 #pragma unroll
-                for (int x = 0; x < kFa; ++x)
+                for (int y = 0; y < kFb; ++y)
 #pragma unroll
-                    for (int y = 0; y < kFb; ++y) acc[x][y] = Elem<T>::mma(fa[x], fb[y], acc[x][y]);
-                if (SUMS)
+                    for (int x = 0; x < kFa; ++x) acc[x][y] = Elem<T>::mma(fa[x], fb[y], acc[x][y]);
+                if (SUMS && with_sums)
 #pragma unroll
-                    for (int y = 0; y < kFb; ++y) sums[y] = Elem<T>::mma(Elem<T>::ones(), fb[y], sums[y]);
+                    for (int y = 0; y < kFb; ++y)
+                        if (y / kSums == wave % WA) sums[y % kSums] = Elem<T>::mma(Elem<T>::ones(), fb[y], sums[y % kSums]);
             }
         };
-        // every wavefront's loads have landed, then all have arrived (a barrier alone does not wait for loads to LDS)
-        const auto meet = [&]() {
-            if (ASYNC) __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
-            __syncthreads();
-        };
         if (limit <= 0) return;
-        a.ask(a0, 0, tid);
-        b.ask(b0, 0, tid);
         a.put(a0, tid);
         b.put(b0, tid);
         meet();
         // two stages a round, so that each has its own half of LDS by name: loads into one go on under the products of the other
-        for (int32_t k = 0;;) {
-            if (k + kBk < limit) { a.ask(a1, k + kBk, tid); b.ask(b1, k + kBk, tid); }
+        for (int32_t k = 0; k < limit; k += 2 * kBk) {
+            const bool second = k + kBk < limit, third = k + 2 * kBk < limit;
+            if (second) { a.ask(a1, k + kBk, tid); b.ask(b1, k + kBk, tid); }
             step(a0, b0);
-            if ((k += kBk) >= limit) break;
-            a.put(a1, tid);
-            b.put(b1, tid);
+            if (second) { a.put(a1, tid); b.put(b1, tid); }
             meet();
-            if (k + kBk < limit) { a.ask(a0, k + kBk, tid); b.ask(b0, k + kBk, tid); }
-            step(a1, b1);
-            if ((k += kBk) >= limit) break;
-            a.put(a0, tid);
-            b.put(b0, tid);
+            if (third) { a.ask(a0, k + 2 * kBk, tid); b.ask(b0, k + 2 * kBk, tid); }
+            if (second) step(a1, b1);
+            if (third) { a.put(a0, tid); b.put(b0, tid); }
             meet();
         }
     }
 };
+
+// The items of a launch in eight runs, one an XCD (consecutive workgroups go to the eight XCDs in turn), whose workgroups take a run's
+// items in turn: what an XCD works on at one time are neighbours, which share operands in its L2.
+struct Deal { int64_t at, stop, step; };
+__device__ __forceinline__ Deal my_items(int64_t total) {
+    const int64_t blocks = (int64_t)gridDim.x * gridDim.y, b = block_number();
+    if (blocks % 8) return Deal{b, total, blocks};
+    const int64_t xcd = b & 7, from = total * xcd / 8, to = total * (xcd + 1) / 8;
+    return Deal{from + (b >> 3), to, blocks >> 3};
+}
 
 struct ProductArgs {
     const int32_t* offsets;
@@ -378,94 +458,166 @@ struct ProductArgs {
     int64_t z_stride;
     int64_t rows;
     int32_t n_groups, in, out, activation;
-    int32_t whole_stores;        // y, z_out and slope_at take four columns at a time
 };
 
-template <typename O>
-__device__ __forceinline__ void store4(O* to, const float* v, int n, bool whole) {
-    if (whole) {
-        O part[4];
+// The first n of N columns to memory, one by one (results whose rows are not made of whole 16 bytes)
+template <typename O, int N>
+__device__ __forceinline__ void store_columns(O* to, const float* v, int n) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) part[i] = (O)v[i];
-        struct alignas(4 * sizeof(O)) Four { O v[4]; };
-        *(Four*)to = *(Four*)part;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < n) to[i] = (O)v[i];
-    }
+    for (int i = 0; i < N; ++i)
+        if (i < n) to[i] = (O)v[i];
 }
 
-// y = act(x W^T + b), or (x W^T) act'(z).  One workgroup a tile of TB rows and TA columns; consecutive workgroups of an XCD take
-// the column tiles of one row tile after the other, so that x is read from memory once and a group's weights stay in its L2.
-template <typename T, typename O, int TA, int TB, int WA, int WB, bool W_KC, bool ASYNC>
-__global__ void __launch_bounds__(64 * WA * WB) k_grouped_product(ProductArgs p) {
-    typedef Tile<T, TA, TB, WA, WB, W_KC, true, ASYNC> Work;
-    __shared__ uint4 a0[TA * kTileChunks], a1[TA * kTileChunks], b0[TB * kTileChunks], b1[TB * kTileChunks];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int32_t across = (p.out + TA - 1) / TA;
-    const int64_t total = (int64_t)count_items(p.offsets, p.n_groups, p.rows, TB, 0, true, lane) * across;
-    const int64_t block = block_number();
-    const int64_t per = (total + 7) / 8, turn = block >> 3;
-    const int64_t at = (block & 7) * per + turn;
-    if (turn >= per || at >= total) return;
-    const Item it = find_item(p.offsets, p.n_groups, p.rows, TB, 0, true, (int32_t)(at / across), lane);
-    const int32_t a_first = (int32_t)(at % across) * TA;
-    const int64_t b_first = it.begin + (int64_t)it.index * TB;
-    const int32_t count = (int32_t)(it.end - b_first < TB ? it.end - b_first : TB);
-    Work work;
-    f32x4 none[1];
-    if (it.group < p.n_groups) {
-        typename Work::A a;
-        typename Work::B b;
-        const Source w{(const T*)p.w + (int64_t)it.group * p.w_group, p.w_stride, nullptr, 0, 1};
-        if (W_KC) a.open_rows(w, a_first, p.out - a_first, p.in, tid);
-        else a.open_columns(w, 0, p.in, a_first, p.out);
-        b.open_rows(p.x, b_first, count, p.in, tid);
-        work.template run<false>(a, b, a0, b0, a1, b1, p.in, none, tid);
-    } else {
+// A wavefront's 16 rows of finished values to memory in whole rows: a matrix instruction leaves 16 consecutive lanes with 16
+// rows, and stores go out 16 lanes at a time, so rows pass through LDS first and leave 128 bytes and more side by side (pieces of 16 bytes
+// straight from the registers were written to memory 1.4 times, and a large product took 15 % longer).  They pass the caches by:
+// a later kernel reads them.
+template <typename W, typename X>
+struct Rows16 {
+    static constexpr int kCols = 16 * W::kFa, kChunks = kCols * (int)sizeof(X) / 16, kMask = (kChunks < 8 ? kChunks : 8) - 1;
+    static __device__ __forceinline__ void put(char* patch, int set, const float* v, int lane) {   // the lane's piece of its row
+        constexpr int n = W::kN * (int)sizeof(X) > 16 ? 16 / (int)sizeof(X) : W::kN;   // values at a time: 16 bytes or a part of them
+        const int row = lane & 15;
 #pragma unroll
-        for (int x = 0; x < Work::kFa; ++x)
+        for (int j = 0; j < W::kN; j += n) {
+            X part[n];
 #pragma unroll
-            for (int y = 0; y < Work::kFb; ++y) work.acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < n; ++i) part[i] = (X)v[j + i];
+            const int byte = (16 * W::kQ * set + W::kN * (lane >> 4) + j) * (int)sizeof(X);
+            __builtin_memcpy(__builtin_assume_aligned(patch + row * kCols * (int)sizeof(X) + (((byte >> 4) ^ (row & kMask)) << 4) + (byte & 15), sizeof(part)), part, sizeof(part));
+        }
     }
-    const bool inside = it.group < p.n_groups;
-    const int wa = (wave % WA) * (TA / WA), wb = (wave / WA) * (TB / WB), g = lane >> 4, i = lane & 15;
+    // rows 0 .. count - 1 of the 16, columns below `columns` from `to` on
+    static __device__ __forceinline__ void send(const char* patch, X* to, int64_t stride, int count, int columns, int lane) {
+        typedef uint32_t Word __attribute__((ext_vector_type(4)));
 #pragma unroll
-    for (int x = 0; x < Work::kFa; ++x) {
-        const int32_t col = a_first + wa + 16 * x + 4 * g;
-        const int n = p.out - col;
-        if (n <= 0) continue;
-        const bool whole = p.whole_stores && n >= 4;
-        float bias[4] = {0.f, 0.f, 0.f, 0.f};
-        if (p.bias && inside) {
-            const T* from = (const T*)p.bias + (int64_t)it.group * p.bias_stride + col;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j < n) bias[j] = (float)from[j];
-        }
-#pragma unroll
-        for (int y = 0; y < Work::kFb; ++y) {
-            const int r = wb + 16 * y + i;
-            if (r >= count) continue;
-            const int64_t row = b_first + r;
-            float v[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = work.acc[x][y][j] + bias[j];
-            if (inside && p.slope_at) {
-                const T* z = (const T*)p.slope_at + row * p.slope_stride + col;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j < n) v[j] *= activation_slope((float)z[j], p.activation);
-            } else if (inside) {
-                if (p.z_out) store4((T*)p.z_out + row * p.z_stride + col, v, n, whole);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = activate(v[j], p.activation);
-            } else if (p.z_out) {
-                store4((T*)p.z_out + row * p.z_stride + col, v, n, whole);
+        for (int t = 0; t < 16 * kChunks; t += 64) {
+            const int at = t + lane, row = at / kChunks, chunk = at % kChunks;
+            if ((16 * kChunks >= 64 || at < 16 * kChunks) && row < count && chunk * (16 / (int)sizeof(X)) < columns) {
+                const Word w = *(const Word*)(patch + (row * kChunks + (chunk ^ (row & kMask))) * 16);
+                __builtin_nontemporal_store(w, (Word*)(to + row * stride + chunk * (16 / (int)sizeof(X))));
             }
-            store4((O*)p.y + row * p.y_stride + col, v, n, whole);
         }
+    }
+};
+
+// y = act(x W^T + b), or (x W^T) act'(z).  Workgroups stay and take tiles in turn, the column tiles of a row tile next to each
+// other: x comes from memory once, a group's weights stay in the XCD's L2.  The next tile's first stage is asked for before the results
+// of this one are finished and stored.
+// FAST: whole 16-byte chunks on every side (loads straight to LDS, whole stores); otherwise element by element at the ends.
+template <typename T, typename O, int TA, int TB, int WA, int WB, bool W_KC, bool FAST>
+__global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_product(ProductArgs p) {
+    typedef Tile<T, O, TA, TB, WA, WB, W_KC, false, true, true, FAST> Work;
+    constexpr int N = Work::kN;
+    __shared__ uint4 a0[TA * kTileChunks], a1[TA * kTileChunks], b0[TB * kTileChunks], b1[TB * kTileChunks];
+    const int lane = threadIdx.x & 63, tid = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 64 + lane;   // (the wavefront's number in a scalar register)
+    const int32_t across = (p.out + TA - 1) / TA;
+    Deal deal = my_items((int64_t)count_items(p.offsets, p.n_groups, p.rows, TB, 0, true, lane) * across);
+    Work work;
+    typename Work::A a;
+    typename Work::B b;
+    Item it;
+    it.group = -1;
+    // what is in the works: a tile whose first stage has been asked for
+    int32_t row_tile = -1, group = 0, column = 0, count = 0;
+    int64_t first = 0;
+    for (bool have = false;; have = true) {
+        if (have) {
+            // the sums begin with the bias
+#pragma unroll
+            for (int set = 0; set < Work::kSets; ++set) {
+                const int32_t col = column + Work::column(set, tid);
+                const T* from = (const T*)p.bias + (int64_t)group * p.bias_stride + col;
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const float start = p.bias && group < p.n_groups && (FAST ? col : col + j) < p.out ? (float)from[j] : 0.f;
+#pragma unroll
+                    for (int y = 0; y < Work::kFb; ++y) work.at(set, y, j) = start;
+                }
+            }
+            work.template run<false>(a, b, a0, b0, a1, b1, group < p.n_groups ? p.in : 0, nullptr, false, tid);
+        }
+        const int32_t done_group = group, done_column = column, done_count = count;
+        const int64_t done_first = first;
+        const bool more = deal.at < deal.stop;
+        if (more) {
+            const int32_t tile = (int32_t)(deal.at / across);
+            column = (int32_t)(deal.at - (int64_t)tile * across) * TA;
+            if (tile != row_tile) {
+                row_tile = tile;
+                if (it.group < 0 || tile >= it.first + it.items) it = find_item(p.offsets, p.n_groups, p.rows, TB, 0, true, tile, lane);
+                group = it.group;
+                first = it.begin + (int64_t)(tile - it.first) * TB;
+                count = (int32_t)(it.end - first < TB ? it.end - first : TB);
+                b.open_rows(p.x, first, count, p.in, tid);
+            }
+            if (group < p.n_groups) {
+                const Source w{(const T*)p.w + (int64_t)group * p.w_group, p.w_stride, nullptr, 0, 1};
+                if (W_KC) a.open_rows(w, column, p.out - column, p.in, tid);
+                else a.open_columns(w, 0, p.in, column, p.out, tid);
+                a.ask(a0, 0, tid);
+                b.ask(b0, 0, tid);
+            }
+            deal.at += deal.step;
+        }
+        if (have) {
+            const bool inside = done_group < p.n_groups;
+            char* patch = Work::patch(a1, b1, tid);
+            const auto finish = [&](auto act, auto slope) {
+                constexpr int ACT = decltype(act)::value, SLOPE = decltype(slope)::value;
+                const int32_t wave_column = done_column + Work::column(0, tid & ~63);
+#pragma unroll
+                for (int y = 0; y < Work::kFb; ++y) {
+                    const int r0 = Work::row(y, tid & ~63), r = Work::row(y, tid);
+                    if (r0 >= done_count) continue;
+                    float v[Work::kSets][N];
+#pragma unroll
+                    for (int set = 0; set < Work::kSets; ++set) {
+                        const int32_t col = done_column + Work::column(set, tid);
+                        const int n = r < done_count ? p.out - col : 0;
+#pragma unroll
+                        for (int j = 0; j < N; ++j) v[set][j] = work.at(set, y, j);
+                        if (SLOPE) {
+                            const T* from = (const T*)p.slope_at + (done_first + r) * p.slope_stride + col;
+                            T z[N];
+                            if (FAST && n > 0) __builtin_memcpy(z, from, sizeof(z));   // (aligned as an element is)
+                            else
+#pragma unroll
+                                for (int j = 0; j < N; ++j) z[j] = j < n ? from[j] : (T)0.f;
+#pragma unroll
+                            for (int j = 0; j < N; ++j) v[set][j] *= activation_slope<ACT>((float)z[j]);
+                        } else if (p.z_out) {
+                            if (FAST) Rows16<Work, T>::put(patch, set, v[set], lane);
+                            else store_columns<T, N>((T*)p.z_out + (done_first + r) * p.z_stride + col, v[set], n);
+                        }
+                    }
+                    if (FAST && !SLOPE && p.z_out)
+                        Rows16<Work, T>::send(patch, (T*)p.z_out + (done_first + r0) * p.z_stride + wave_column, p.z_stride, done_count - r0, p.out - wave_column, lane);
+#pragma unroll
+                    for (int set = 0; set < Work::kSets; ++set) {
+                        if (!SLOPE && inside)
+#pragma unroll
+                            for (int j = 0; j < N; ++j) v[set][j] = activate<ACT>(v[set][j]);
+                        if (FAST) {
+                            Rows16<Work, O>::put(patch, set, v[set], lane);
+                        } else {
+                            const int32_t col = done_column + Work::column(set, tid);
+                            store_columns<O, N>((O*)p.y + (done_first + r) * p.y_stride + col, v[set], r < done_count ? p.out - col : 0);
+                        }
+                    }
+                    if (FAST) Rows16<Work, O>::send(patch, (O*)p.y + (done_first + r0) * p.y_stride + wave_column, p.y_stride, done_count - r0, p.out - wave_column, lane);
+                }
+            };
+            const int act = inside ? p.activation : (int)kNone;   // (one copy of the code for each, outside the loops over rows)
+            if (p.slope_at && act == kRelu) finish(Constant<kRelu>{}, Constant<1>{});
+            else if (p.slope_at && act == kSilu) finish(Constant<kSilu>{}, Constant<1>{});
+            else if (p.slope_at && act == kGelu) finish(Constant<kGelu>{}, Constant<1>{});
+            else if (act == kRelu) finish(Constant<kRelu>{}, Constant<0>{});
+            else if (act == kSilu) finish(Constant<kSilu>{}, Constant<0>{});
+            else if (act == kGelu) finish(Constant<kGelu>{}, Constant<0>{});
+            else finish(Constant<kNone>{}, Constant<0>{});
+        }
+        if (!more) break;
     }
 }
 
@@ -474,52 +626,194 @@ struct GradientArgs {
     Source x, dy;            // x: [.., in], gathered; dy: [rows, out]
     void* dw;                // [n_groups, out, in]
     float* db;               // NULL or [n_groups, out]
+    float* part;             // [slots][out, in] sums of parts of long groups, behind them [slots][out] of db
+    int64_t slots;
     int64_t rows;
     int32_t n_groups, in, out;
-    int32_t whole_stores;
+    int32_t most;            // rows a part has at most
 };
 
-// dW = sum over the group's rows of dy^T x: one workgroup a tile of TA columns of x and TB of dy.
-template <typename T, typename O, int TA, int TB, int WA, int WB, bool ASYNC>
-__global__ void __launch_bounds__(64 * WA * WB) k_grouped_gradient(GradientArgs p) {
-    typedef Tile<T, TA, TB, WA, WB, false, false, ASYNC> Work;
+// A group of more than `most` rows is taken in parts of equal length (at least most / 2 rows), so that no workgroup has much more to do than the
+// others; their sums meet in k_grouped_parts, always in the same order.
+__device__ __forceinline__ int32_t parts_of(int64_t count, int32_t most) { return count <= most ? 1 : (int32_t)((count + most - 1) / most); }
+__device__ __forceinline__ int64_t part_begin(int64_t begin, int64_t count, int32_t part, int32_t parts) { return begin + count * part / parts; }
+// Parts of long groups begin at least most / 2 rows apart: the place for their sums
+__device__ __forceinline__ int64_t slot_of(int64_t part_begin, int32_t most) { return part_begin / (most / 2); }
+
+struct Unit {
+    int64_t begin;
+    int32_t group, count, parts;
+};
+// Parts in the order in which they are taken: long ones first (four classes by length), so that what is left at the end is short.
+// Number `at` of them, or, with group -1 beyond the last, their number in `parts`.
+__device__ __forceinline__ Unit find_unit(const GradientArgs& p, int32_t at, int lane) {
+    int32_t before = 0;
+    for (int32_t length = 0; length < 4; ++length)
+        for (int32_t g0 = 0; g0 < p.n_groups; g0 += 64) {
+            const int32_t e = g0 + lane;
+            int64_t begin = 0, count = 0;
+            int32_t parts = 0, mine = 0;
+            if (e < p.n_groups) {
+                begin = group_end(p.offsets, e, p.n_groups, p.rows);
+                count = group_end(p.offsets, e + 1, p.n_groups, p.rows) - begin;
+                if (count < 0) count = 0;
+                parts = parts_of(count, p.most);
+                const int64_t rows = count / parts;
+                const int32_t is = rows * 2 > p.most ? 0 : rows * 4 > p.most ? 1 : rows * 8 > p.most ? 2 : 3;
+                if (is == length) mine = parts;
+            }
+            const int32_t upto = before + wave_inclusive(mine, lane);
+            const uint64_t mask = __ballot(upto > at);
+            if (mask) {
+                const int who = __builtin_ctzll(mask);
+                const int64_t b = of_lane(begin, who), c = of_lane(count, who);
+                Unit u;
+                u.parts = of_lane(parts, who);
+                const int32_t part = at - of_lane(upto - mine, who);
+                u.group = g0 + who;
+                u.begin = part_begin(b, c, part, u.parts);
+                u.count = (int32_t)(part_begin(b, c, part + 1, u.parts) - u.begin);
+                return u;
+            }
+            before = of_lane(upto, 63);
+        }
+    return Unit{0, -1, 0, before};
+}
+
+// dW = sum over the group's rows of dy^T x: tiles of TA columns of x and TB of dy.  The tiles of a part go to one XCD, side by side: they read
+// the same rows.  Workgroups stay and take every so many-th tile of their XCD, in turn from either end, as the parts get shorter.
+template <typename T, typename O, int TA, int TB, int WA, int WB, bool FAST>
+__global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_gradient(GradientArgs p) {
+    typedef Tile<T, O, TA, TB, WA, WB, false, true, false, false, FAST> Work;
+    constexpr int N = Work::kN;
     __shared__ uint4 a0[TA * kTileChunks], a1[TA * kTileChunks], b0[TB * kTileChunks], b1[TB * kTileChunks];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int32_t across = (p.in + TA - 1) / TA, down = (p.out + TB - 1) / TB;
-    const int64_t block = block_number(), tiles = (int64_t)across * down;
-    if (block >= p.n_groups * tiles) return;
-    const int64_t tile = block % tiles;
-    const int32_t group = (int32_t)(block / tiles);
-    const int64_t begin = group_end(p.offsets, group, p.n_groups, p.rows), stop = group_end(p.offsets, group + 1, p.n_groups, p.rows);
-    const int32_t count = stop > begin ? (int32_t)(stop - begin) : 0;
-    const int32_t a_first = (int32_t)(tile % across) * TA, b_first = (int32_t)(tile / across) * TB;
+    const int lane = threadIdx.x & 63, tid = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 64 + lane;   // (the wavefront's number in a scalar register)
+    const int32_t across = (p.in + TA - 1) / TA, tiles = across * ((p.out + TB - 1) / TB);
+    const int32_t units = find_unit(p, 0x7fffffff, lane).parts;
+    const int32_t xcds = gridDim.x % 8 == 0 ? 8 : 1, xcd = (int32_t)blockIdx.x % xcds, local = (int32_t)blockIdx.x / xcds, locals = (int32_t)gridDim.x / xcds;
     Work work;
     typename Work::A a;
     typename Work::B b;
-    a.open_columns(p.x, begin, count, a_first, p.in);
-    b.open_columns(p.dy, begin, count, b_first, p.out);
-    f32x4 sums[Work::kFb];
+    Unit unit{0, -1, 0, 0};
+    int32_t unit_at = -1, a_first = 0, b_first = 0;
+    int32_t turn = 0;
+    for (bool have = false;; have = true) {
+        f32x4 sums[Work::kSums];
+        const bool bias = have && p.db && a_first == 0;
+        if (have) {
+            work.clear();
 #pragma unroll
-    for (int y = 0; y < Work::kFb; ++y) sums[y] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const bool bias = p.db && a_first == 0;
-    if (bias) work.template run<true>(a, b, a0, b0, a1, b1, count, sums, tid);
-    else work.template run<false>(a, b, a0, b0, a1, b1, count, sums, tid);
-    const int wa = (wave % WA) * (TA / WA), wb = (wave / WA) * (TB / WB), g = lane >> 4, i = lane & 15;
-#pragma unroll
-    for (int y = 0; y < Work::kFb; ++y) {
-        const int32_t r = b_first + wb + 16 * y + i;
-        if (r >= p.out) continue;
-        if (bias && wave % WA == 0 && g == 0) p.db[(int64_t)group * p.out + r] = sums[y][0];
-#pragma unroll
-        for (int x = 0; x < Work::kFa; ++x) {
-            const int32_t col = a_first + wa + 16 * x + 4 * g;
-            const int n = p.in - col;
-            if (n <= 0) continue;
-            float v[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = work.acc[x][y][j];
-            store4((O*)p.dw + ((int64_t)group * p.out + r) * p.in + col, v, n, p.whole_stores && n >= 4);
+            for (int y = 0; y < Work::kSums; ++y) sums[y] = f32x4{0.f, 0.f, 0.f, 0.f};
+            work.template run<true>(a, b, a0, b0, a1, b1, unit.count, sums, bias, tid);
         }
+        const Unit done = unit;
+        const int32_t done_a = a_first, done_b = b_first;
+        // the next tile: number t of this XCD's
+        const int64_t t = (int64_t)turn * locals + (turn & 1 ? locals - 1 - local : local), band = t / tiles;
+        const int64_t next = band * xcds + (band & 1 ? xcds - 1 - xcd : xcd);
+        ++turn;
+        const bool more = next < units;
+        if (more) {
+            const int32_t tile = (int32_t)(t - band * tiles);
+            if (next != unit_at) unit = find_unit(p, (int32_t)next, lane);
+            unit_at = (int32_t)next;
+            a_first = tile % across * TA;
+            b_first = tile / across * TB;
+            a.open_columns(p.x, unit.begin, unit.count, a_first, p.in, tid);
+            b.open_columns(p.dy, unit.begin, unit.count, b_first, p.out, tid);
+            if (unit.count > 0) {
+                a.ask(a0, 0, tid);
+                b.ask(b0, 0, tid);
+            }
+        }
+        if (have) {
+            const int64_t slot = slot_of(done.begin, p.most);
+            if (bias && lane < 16) {
+                float* to = done.parts == 1 ? p.db + (int64_t)done.group * p.out : p.part + p.slots * p.out * p.in + slot * p.out;
+#pragma unroll
+                for (int y = 0; y < Work::kFb; ++y) {
+                    const int32_t r = done_b + Work::row(y, tid);
+                    if (Work::sums_of(y, tid) && r < p.out) to[r] = sums[y % Work::kSums][0];
+                }
+            }
+            char* patch = Work::patch(a1, b1, tid);
+            const int32_t wave_column = done_a + Work::column(0, tid & ~63);
+            const auto out = [&](auto* to) {
+                typedef typename std::remove_pointer<decltype(to)>::type X;
+#pragma unroll
+                for (int y = 0; y < Work::kFb; ++y) {
+                    const int32_t r0 = done_b + Work::row(y, tid & ~63), r = done_b + Work::row(y, tid);
+                    if (r0 >= p.out) continue;
+#pragma unroll
+                    for (int set = 0; set < Work::kSets; ++set) {
+                        const int32_t col = done_a + Work::column(set, tid);
+                        float v[N];
+#pragma unroll
+                        for (int j = 0; j < N; ++j) v[j] = work.at(set, y, j);
+                        if (FAST) Rows16<Work, X>::put(patch, set, v, lane);
+                        else store_columns<X, N>(to + (int64_t)r * p.in + col, v, r < p.out ? p.in - col : 0);
+                    }
+                    if (FAST) Rows16<Work, X>::send(patch, to + (int64_t)r0 * p.in + wave_column, p.in, p.out - r0, p.in - wave_column, lane);
+                }
+            };
+            if (done.parts == 1) out((O*)p.dw + (int64_t)done.group * p.out * p.in);
+            else out(p.part + slot * p.out * p.in);
+        }
+        if (!more) break;
+    }
+}
+
+// The sums of the parts of long groups: a workgroup takes 4,096 elements of one
+constexpr int kPiece = 4096;
+template <typename O>
+__global__ void __launch_bounds__(256) k_grouped_parts(GradientArgs p) {
+    const int64_t size = (int64_t)p.out * p.in, pieces = (size + kPiece - 1) / kPiece, block = block_number();
+    const int64_t number = block / pieces, piece = block - number * pieces;
+    const int lane = threadIdx.x & 63;
+    // long group `number`
+    int32_t group = -1, before = 0;
+    int64_t begin = 0, count = 0;
+    for (int32_t g0 = 0; g0 < p.n_groups; g0 += 64) {
+        const int32_t e = g0 + lane;
+        if (e < p.n_groups) {
+            begin = group_end(p.offsets, e, p.n_groups, p.rows);
+            count = group_end(p.offsets, e + 1, p.n_groups, p.rows) - begin;
+        }
+        const uint64_t mask = __ballot(e < p.n_groups && count > p.most);
+        const int found = __popcll(mask);
+        if (number < before + found) {
+            uint64_t left = mask;
+            for (int64_t j = before; j < number; ++j) left &= left - 1;
+            const int who = __builtin_ctzll(left);
+            group = g0 + who;
+            begin = of_lane(begin, who);
+            count = of_lane(count, who);
+            break;
+        }
+        before += found;
+    }
+    if (group < 0) return;
+    const int32_t parts = parts_of(count, p.most);
+    const float* biases = p.part + p.slots * size;
+    if (p.db && piece == 0)
+        for (int32_t r = threadIdx.x; r < p.out; r += 256) {
+            float sum = 0.f;
+            for (int32_t j = 0; j < parts; ++j) sum += biases[slot_of(part_begin(begin, count, j, parts), p.most) * p.out + r];
+            p.db[(int64_t)group * p.out + r] = sum;
+        }
+    float sum[kPiece / 256] = {};
+    for (int32_t j = 0; j < parts; ++j) {
+        const float* from = p.part + slot_of(part_begin(begin, count, j, parts), p.most) * size;
+#pragma unroll
+        for (int q = 0; q < kPiece / 256; ++q) {
+            const int64_t i = piece * kPiece + q * 256 + threadIdx.x;
+            if (i < size) sum[q] += from[i];
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < kPiece / 256; ++q) {
+        const int64_t i = piece * kPiece + q * 256 + threadIdx.x;
+        if (i < size) ((O*)p.dw)[(int64_t)group * size + i] = (O)sum[q];
     }
 }
 
