@@ -67,16 +67,16 @@ extern "C" int nomad_grouped_product(const nomad_grouped_product_args* args) {
     p.in = a.in;
     p.out = a.out;
     p.activation = a.activation;
-    // loads straight to LDS take 16 aligned bytes, stores too: every row of every side begins and ends on such a border
-    const bool fast = by(a.x, a.x_stride, size, 16) && by(a.w, a.w_group_stride, size, 16) && by(a.w, p.w_stride, size, 16) && a.in % chunk == 0 && a.out % chunk == 0 &&
-                      by(a.y, a.y_stride, out_size, 16) && (!a.z_out || by(a.z_out, a.z_stride, size, 16));
+    // loads straight to LDS take 16 aligned bytes, and so do whole stores: rows begin and end on such a border
+    const bool loads = by(a.x, a.x_stride, size, 16) && by(a.w, a.w_group_stride, size, 16) && by(a.w, p.w_stride, size, 16) && a.in % chunk == 0 && (w_kc || a.out % chunk == 0);
+    const bool stores = by(a.y, a.y_stride, out_size, 16) && a.out % (16 / out_size) == 0 && (!a.z_out || (by(a.z_out, a.z_stride, size, 16) && a.out % chunk == 0));
     const int units = units_of(a.device);
     if (units < 1) return NOMAD_E_HIP;
     const bool wide = a.out_dtype != a.dtype;
-    const ProductTile tile = plan_product(a.rows, a.n_groups, a.in, a.out, size == 2, units);
-    if (a.dtype == NOMAD_F32) product_f32(p, tile, wide, w_kc, fast, units, st);
-    else if (a.dtype == NOMAD_BF16) product_bf16(p, tile, wide, w_kc, fast, units, st);
-    else product_f16(p, tile, wide, w_kc, fast, units, st);
+    const ProductTile tile = plan_product(a.rows, a.n_groups, a.out, size == 2, w_kc, units);
+    if (a.dtype == NOMAD_F32) product_f32(p, tile, wide, w_kc, loads, stores, units, st);
+    else if (a.dtype == NOMAD_BF16) product_bf16(p, tile, wide, w_kc, loads, stores, units, st);
+    else product_f16(p, tile, wide, w_kc, loads, stores, units, st);
     KTRY(hipGetLastError());
     return NOMAD_OK;
 }
@@ -113,14 +113,16 @@ extern "C" int nomad_grouped_weight_gradient(const nomad_grouped_gradient_args* 
     const GradientPlan plan = plan_gradient(a.rows, a.n_groups, a.in, a.out, size == 2, kPlanUnits);
     p.part = (float*)a.workspace;
     p.most = plan.most;
+    p.slot_bits = plan.slot_bits;
     p.slots = plan.slots;
-    const bool fast = by(a.x, a.x_stride, size, 16) && by(a.dy, a.dy_stride, size, 16) && a.in % chunk == 0 && a.out % chunk == 0 && by(a.dw, a.in, out_size, 16);
+    const bool loads = by(a.x, a.x_stride, size, 16) && by(a.dy, a.dy_stride, size, 16) && a.in % chunk == 0 && a.out % chunk == 0;
+    const bool stores = by(a.dw, a.in, out_size, 16) && a.in % 4 == 0;   // (sums of parts are stored 16 bytes at a time too)
     const int units = units_of(a.device);
     if (units < 1) return NOMAD_E_HIP;
     const bool wide = a.out_dtype != a.dtype;
-    if (a.dtype == NOMAD_F32) gradient_f32(p, plan, wide, fast, units, st);
-    else if (a.dtype == NOMAD_BF16) gradient_bf16(p, plan, wide, fast, units, st);
-    else gradient_f16(p, plan, wide, fast, units, st);
+    if (a.dtype == NOMAD_F32) gradient_f32(p, plan, wide, loads, stores, units, st);
+    else if (a.dtype == NOMAD_BF16) gradient_bf16(p, plan, wide, loads, stores, units, st);
+    else gradient_f16(p, plan, wide, loads, stores, units, st);
     KTRY(hipGetLastError());
     return NOMAD_OK;
 }

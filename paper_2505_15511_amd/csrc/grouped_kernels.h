@@ -504,10 +504,11 @@ struct Rows16 {
 // y = act(x W^T + b), or (x W^T) act'(z).  Workgroups stay and take tiles in turn, the column tiles of a row tile next to each
 // other: x comes from memory once, a group's weights stay in the XCD's L2.  The next tile's first stage is asked for before the results
 // of this one are finished and stored.
-// FAST: whole 16-byte chunks on every side (loads straight to LDS, whole stores); otherwise element by element at the ends.
-template <typename T, typename O, int TA, int TB, int WA, int WB, bool W_KC, bool FAST>
+// LOADS, STORES: rows are made of whole aligned 16-byte chunks where they are read (straight to LDS), where they are written; otherwise
+// element by element at the ends.
+template <typename T, typename O, int TA, int TB, int WA, int WB, bool W_KC, bool LOADS, bool STORES>
 __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_product(ProductArgs p) {
-    typedef Tile<T, O, TA, TB, WA, WB, W_KC, false, true, true, FAST> Work;
+    typedef Tile<T, O, TA, TB, WA, WB, W_KC, false, true, true, LOADS> Work;
     constexpr int N = Work::kN;
     __shared__ uint4 a0[TA * kTileChunks], a1[TA * kTileChunks], b0[TB * kTileChunks], b1[TB * kTileChunks];
     const int lane = threadIdx.x & 63, tid = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 64 + lane;   // (the wavefront's number in a scalar register)
@@ -530,7 +531,7 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_product(ProductArgs
                 const T* from = (const T*)p.bias + (int64_t)group * p.bias_stride + col;
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    const float start = p.bias && group < p.n_groups && (FAST ? col : col + j) < p.out ? (float)from[j] : 0.f;
+                    const float start = p.bias && group < p.n_groups && (STORES ? col : col + j) < p.out ? (float)from[j] : 0.f;
 #pragma unroll
                     for (int y = 0; y < Work::kFb; ++y) work.at(set, y, j) = start;
                 }
@@ -580,32 +581,32 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_product(ProductArgs
                         if (SLOPE) {
                             const T* from = (const T*)p.slope_at + (done_first + r) * p.slope_stride + col;
                             T z[N];
-                            if (FAST && n > 0) __builtin_memcpy(z, from, sizeof(z));   // (aligned as an element is)
+                            if (STORES && n > 0) __builtin_memcpy(z, from, sizeof(z));   // (aligned as an element is)
                             else
 #pragma unroll
                                 for (int j = 0; j < N; ++j) z[j] = j < n ? from[j] : (T)0.f;
 #pragma unroll
                             for (int j = 0; j < N; ++j) v[set][j] *= activation_slope<ACT>((float)z[j]);
                         } else if (p.z_out) {
-                            if (FAST) Rows16<Work, T>::put(patch, set, v[set], lane);
+                            if (STORES) Rows16<Work, T>::put(patch, set, v[set], lane);
                             else store_columns<T, N>((T*)p.z_out + (done_first + r) * p.z_stride + col, v[set], n);
                         }
                     }
-                    if (FAST && !SLOPE && p.z_out)
+                    if (STORES && !SLOPE && p.z_out)
                         Rows16<Work, T>::send(patch, (T*)p.z_out + (done_first + r0) * p.z_stride + wave_column, p.z_stride, done_count - r0, p.out - wave_column, lane);
 #pragma unroll
                     for (int set = 0; set < Work::kSets; ++set) {
                         if (!SLOPE && inside)
 #pragma unroll
                             for (int j = 0; j < N; ++j) v[set][j] = activate<ACT>(v[set][j]);
-                        if (FAST) {
+                        if (STORES) {
                             Rows16<Work, O>::put(patch, set, v[set], lane);
                         } else {
                             const int32_t col = done_column + Work::column(set, tid);
                             store_columns<O, N>((O*)p.y + (done_first + r) * p.y_stride + col, v[set], r < done_count ? p.out - col : 0);
                         }
                     }
-                    if (FAST) Rows16<Work, O>::send(patch, (O*)p.y + (done_first + r0) * p.y_stride + wave_column, p.y_stride, done_count - r0, p.out - wave_column, lane);
+                    if (STORES) Rows16<Work, O>::send(patch, (O*)p.y + (done_first + r0) * p.y_stride + wave_column, p.y_stride, done_count - r0, p.out - wave_column, lane);
                 }
             };
             const int act = inside ? p.activation : (int)kNone;   // (one copy of the code for each, outside the loops over rows)
@@ -621,6 +622,78 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_product(ProductArgs
     }
 }
 
+// The same for few rows, where the groups' weights are read once and there are too few tiles for all compute units: a workgroup takes 16
+// rows and 16 columns, its wavefronts share k, two steps (128 bytes of every row) at a time, straight from memory to
+// registers, and add up in LDS.  Latency is all it costs: one row of bfloat16 through two experts of 768 x 2,048 takes 7 us, 15 in
+// tiles of 128.
+constexpr int kFewWaves = 8;
+template <typename T, typename O>
+__global__ void __launch_bounds__(64 * kFewWaves) k_grouped_few(ProductArgs p) {
+    constexpr int epc = 16 / (int)sizeof(T), step = 4 * epc;   // k a step: a chunk for every lane group
+    __shared__ f32x4 part[kFewWaves][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4, i = lane & 15;
+    const int32_t across = (p.out + 15) / 16;
+    const int64_t block = block_number();
+    const int32_t tile = (int32_t)(block / across), column = (int32_t)(block - (int64_t)tile * across) * 16;
+    const Item it = find_item(p.offsets, p.n_groups, p.rows, 16, 0, true, tile, lane);
+    if (it.group < 0) return;
+    const int64_t first = it.begin + (int64_t)it.index * 16;
+    const int32_t count = (int32_t)(it.end - first < 16 ? it.end - first : 16);
+    const bool inside = it.group < p.n_groups;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    if (inside) {
+        const int64_t at = i < count ? p.x.row_of(first + i) : -1;
+        const T* x = at >= 0 ? (const T*)p.x.base + at * p.x.stride : nullptr;
+        const T* w = column + i < p.out ? (const T*)p.w + (int64_t)it.group * p.w_group + (int64_t)(column + i) * p.w_stride : nullptr;
+        const auto chunk = [&](const T* row, int32_t k) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            const int n = row ? p.in - k : 0;
+            if (n >= epc) {
+                __builtin_memcpy(&v, row + k, 16);   // (aligned as an element is)
+            } else if (n > 0) {
+                T some[epc] = {};
+#pragma unroll
+                for (int j = 0; j < epc; ++j)
+                    if (j < n) some[j] = row[k + j];
+                __builtin_memcpy(&v, some, 16);
+            }
+            return v;
+        };
+        for (int32_t k0 = wave * 2 * step; k0 < p.in; k0 += kFewWaves * 2 * step * 2) {   // four steps on their way at once
+            uint4 a[4], b[4];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const int32_t k = k0 + (s & 1) * step + (s >> 1) * kFewWaves * 2 * step + g * epc;
+                a[s] = chunk(w, k);
+                b[s] = chunk(x, k);
+            }
+#pragma unroll
+            for (int s = 0; s < 4; ++s) acc = Elem<T>::mma(a[s], b[s], acc);
+        }
+    }
+    part[wave][lane] = acc;
+    __syncthreads();
+    if (wave > 0 || i >= count) return;
+#pragma unroll
+    for (int j = 1; j < kFewWaves; ++j) acc += part[j][lane];
+    const int64_t row = first + i;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int32_t col = column + 4 * g + j;
+        if (col >= p.out) break;
+        float v = acc[j];
+        if (inside && p.slope_at) {
+            const float z = (float)((const T*)p.slope_at)[row * p.slope_stride + col];
+            v *= p.activation == kRelu ? activation_slope<kRelu>(z) : p.activation == kSilu ? activation_slope<kSilu>(z) : p.activation == kGelu ? activation_slope<kGelu>(z) : 1.f;
+        } else {
+            if (inside && p.bias) v += (float)((const T*)p.bias)[(int64_t)it.group * p.bias_stride + col];
+            if (p.z_out) ((T*)p.z_out)[row * p.z_stride + col] = (T)v;
+            if (inside) v = p.activation == kRelu ? activate<kRelu>(v) : p.activation == kSilu ? activate<kSilu>(v) : p.activation == kGelu ? activate<kGelu>(v) : v;
+        }
+        ((O*)p.y)[row * p.y_stride + col] = (O)v;
+    }
+}
+
 struct GradientArgs {
     const int32_t* offsets;
     Source x, dy;            // x: [.., in], gathered; dy: [rows, out]
@@ -631,14 +704,18 @@ struct GradientArgs {
     int64_t rows;
     int32_t n_groups, in, out;
     int32_t most;            // rows a part has at most
+    int32_t slot_bits;
 };
 
 // A group of more than `most` rows is taken in parts of equal length (at least most / 2 rows), so that no workgroup has much more to do than the
 // others; their sums meet in k_grouped_parts, always in the same order.
-__device__ __forceinline__ int32_t parts_of(int64_t count, int32_t most) { return count <= most ? 1 : (int32_t)((count + most - 1) / most); }
-__device__ __forceinline__ int64_t part_begin(int64_t begin, int64_t count, int32_t part, int32_t parts) { return begin + count * part / parts; }
-// Parts of long groups begin at least most / 2 rows apart: the place for their sums
-__device__ __forceinline__ int64_t slot_of(int64_t part_begin, int32_t most) { return part_begin / (most / 2); }
+__device__ __forceinline__ int32_t parts_of(int32_t count, int32_t most) { return count <= most ? 1 : (int32_t)(((uint32_t)count + (uint32_t)most - 1) / (uint32_t)most); }
+__device__ __forceinline__ int64_t part_begin(int64_t begin, int32_t count, int32_t part, int32_t parts) {
+    const uint32_t each = (uint32_t)count / (uint32_t)parts, left = (uint32_t)count - each * (uint32_t)parts;
+    return begin + (int64_t)part * each + ((uint32_t)part < left ? (uint32_t)part : left);
+}
+// Parts of long groups begin at least most / 2 rows apart, and 2^slot_bits is no more: the place for their sums
+__device__ __forceinline__ int64_t slot_of(int64_t part_begin, int32_t slot_bits) { return part_begin >> slot_bits; }
 
 struct Unit {
     int64_t begin;
@@ -651,22 +728,23 @@ __device__ __forceinline__ Unit find_unit(const GradientArgs& p, int32_t at, int
     for (int32_t length = 0; length < 4; ++length)
         for (int32_t g0 = 0; g0 < p.n_groups; g0 += 64) {
             const int32_t e = g0 + lane;
-            int64_t begin = 0, count = 0;
-            int32_t parts = 0, mine = 0;
+            int64_t begin = 0;
+            int32_t count = 0, parts = 0, mine = 0;
             if (e < p.n_groups) {
                 begin = group_end(p.offsets, e, p.n_groups, p.rows);
-                count = group_end(p.offsets, e + 1, p.n_groups, p.rows) - begin;
-                if (count < 0) count = 0;
+                const int64_t rows = group_end(p.offsets, e + 1, p.n_groups, p.rows) - begin;
+                count = rows < 0 ? 0 : (int32_t)rows;
                 parts = parts_of(count, p.most);
-                const int64_t rows = count / parts;
-                const int32_t is = rows * 2 > p.most ? 0 : rows * 4 > p.most ? 1 : rows * 8 > p.most ? 2 : 3;
+                // (a part of a long group has more than half of `most` rows)
+                const int32_t is = parts > 1 || count > p.most / 2 ? 0 : count > p.most / 4 ? 1 : count > p.most / 8 ? 2 : 3;
                 if (is == length) mine = parts;
             }
             const int32_t upto = before + wave_inclusive(mine, lane);
             const uint64_t mask = __ballot(upto > at);
             if (mask) {
                 const int who = __builtin_ctzll(mask);
-                const int64_t b = of_lane(begin, who), c = of_lane(count, who);
+                const int64_t b = of_lane(begin, who);
+                const int32_t c = of_lane(count, who);
                 Unit u;
                 u.parts = of_lane(parts, who);
                 const int32_t part = at - of_lane(upto - mine, who);
@@ -682,9 +760,9 @@ __device__ __forceinline__ Unit find_unit(const GradientArgs& p, int32_t at, int
 
 // dW = sum over the group's rows of dy^T x: tiles of TA columns of x and TB of dy.  The tiles of a part go to one XCD, side by side: they read
 // the same rows.  Workgroups stay and take every so many-th tile of their XCD, in turn from either end, as the parts get shorter.
-template <typename T, typename O, int TA, int TB, int WA, int WB, bool FAST>
+template <typename T, typename O, int TA, int TB, int WA, int WB, bool LOADS, bool STORES>
 __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_gradient(GradientArgs p) {
-    typedef Tile<T, O, TA, TB, WA, WB, false, true, false, false, FAST> Work;
+    typedef Tile<T, O, TA, TB, WA, WB, false, true, false, false, LOADS> Work;
     constexpr int N = Work::kN;
     __shared__ uint4 a0[TA * kTileChunks], a1[TA * kTileChunks], b0[TB * kTileChunks], b1[TB * kTileChunks];
     const int lane = threadIdx.x & 63, tid = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 64 + lane;   // (the wavefront's number in a scalar register)
@@ -727,7 +805,7 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_gradient(GradientAr
             }
         }
         if (have) {
-            const int64_t slot = slot_of(done.begin, p.most);
+            const int64_t slot = slot_of(done.begin, p.slot_bits);
             if (bias && lane < 16) {
                 float* to = done.parts == 1 ? p.db + (int64_t)done.group * p.out : p.part + p.slots * p.out * p.in + slot * p.out;
 #pragma unroll
@@ -750,10 +828,10 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_gradient(GradientAr
                         float v[N];
 #pragma unroll
                         for (int j = 0; j < N; ++j) v[j] = work.at(set, y, j);
-                        if (FAST) Rows16<Work, X>::put(patch, set, v, lane);
+                        if (STORES) Rows16<Work, X>::put(patch, set, v, lane);
                         else store_columns<X, N>(to + (int64_t)r * p.in + col, v, r < p.out ? p.in - col : 0);
                     }
-                    if (FAST) Rows16<Work, X>::send(patch, to + (int64_t)r0 * p.in + wave_column, p.in, p.out - r0, p.in - wave_column, lane);
+                    if (STORES) Rows16<Work, X>::send(patch, to + (int64_t)r0 * p.in + wave_column, p.in, p.out - r0, p.in - wave_column, lane);
                 }
             };
             if (done.parts == 1) out((O*)p.dw + (int64_t)done.group * p.out * p.in);
@@ -763,23 +841,24 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_gradient(GradientAr
     }
 }
 
-// The sums of the parts of long groups: a workgroup takes 4,096 elements of one
-constexpr int kPiece = 4096;
+// The sums of the parts of long groups: a workgroup takes 1,024 elements of one
+constexpr int kPiece = 1024;
 template <typename O>
 __global__ void __launch_bounds__(256) k_grouped_parts(GradientArgs p) {
     const int64_t size = (int64_t)p.out * p.in, pieces = (size + kPiece - 1) / kPiece, block = block_number();
     const int64_t number = block / pieces, piece = block - number * pieces;
     const int lane = threadIdx.x & 63;
     // long group `number`
-    int32_t group = -1, before = 0;
-    int64_t begin = 0, count = 0;
+    int32_t group = -1, before = 0, count = 0;
+    int64_t begin = 0;
     for (int32_t g0 = 0; g0 < p.n_groups; g0 += 64) {
         const int32_t e = g0 + lane;
+        int64_t rows = 0;
         if (e < p.n_groups) {
             begin = group_end(p.offsets, e, p.n_groups, p.rows);
-            count = group_end(p.offsets, e + 1, p.n_groups, p.rows) - begin;
+            rows = group_end(p.offsets, e + 1, p.n_groups, p.rows) - begin;
         }
-        const uint64_t mask = __ballot(e < p.n_groups && count > p.most);
+        const uint64_t mask = __ballot(rows > p.most);
         const int found = __popcll(mask);
         if (number < before + found) {
             uint64_t left = mask;
@@ -787,7 +866,7 @@ __global__ void __launch_bounds__(256) k_grouped_parts(GradientArgs p) {
             const int who = __builtin_ctzll(left);
             group = g0 + who;
             begin = of_lane(begin, who);
-            count = of_lane(count, who);
+            count = of_lane((int32_t)rows, who);
             break;
         }
         before += found;
@@ -798,12 +877,12 @@ __global__ void __launch_bounds__(256) k_grouped_parts(GradientArgs p) {
     if (p.db && piece == 0)
         for (int32_t r = threadIdx.x; r < p.out; r += 256) {
             float sum = 0.f;
-            for (int32_t j = 0; j < parts; ++j) sum += biases[slot_of(part_begin(begin, count, j, parts), p.most) * p.out + r];
+            for (int32_t j = 0; j < parts; ++j) sum += biases[slot_of(part_begin(begin, count, j, parts), p.slot_bits) * p.out + r];
             p.db[(int64_t)group * p.out + r] = sum;
         }
     float sum[kPiece / 256] = {};
     for (int32_t j = 0; j < parts; ++j) {
-        const float* from = p.part + slot_of(part_begin(begin, count, j, parts), p.most) * size;
+        const float* from = p.part + slot_of(part_begin(begin, count, j, parts), p.slot_bits) * size;
 #pragma unroll
         for (int q = 0; q < kPiece / 256; ++q) {
             const int64_t i = piece * kPiece + q * 256 + threadIdx.x;

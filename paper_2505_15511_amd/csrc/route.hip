@@ -17,7 +17,7 @@ bool by(const void* p, int64_t stride, int64_t size, int64_t bytes) { return ((u
 // in one than keep the counts well below the logits
 int64_t chunk_rows(int64_t n) { return std::max<int64_t>(256, (n + 1023) / 1024); }
 // One workgroup does it all where the logits are few: the launches of the other form alone take as long
-bool is_small(int64_t n, int32_t n_experts) { return n * n_experts <= 65536 && n <= 1024; }
+bool is_small(int64_t n, int32_t n_experts) { return n * n_experts <= 32768 && n <= 1024; }
 
 template <typename T, int LANES, int K>
 void launch_pick(const RouteArgs& p, bool vec, hipStream_t st) {
@@ -26,22 +26,25 @@ void launch_pick(const RouteArgs& p, bool vec, hipStream_t st) {
     if (vec) hipLaunchKernelGGL((k_route_pick<T, LANES, K, true>), grid, block, lds, st, p);
     else hipLaunchKernelGGL((k_route_pick<T, LANES, K, false>), grid, block, lds, st, p);
 }
-template <typename T, int K>
+template <typename T, int LANES, int K>
 void launch_small(const RouteArgs& p, bool vec, hipStream_t st) {
-    const size_t lds = sizeof(int32_t) * (size_t)p.n_experts;
-    if (vec) hipLaunchKernelGGL((k_route_small<T, K, true>), dim3(1), dim3(kSmallThreads), lds, st, p);
-    else hipLaunchKernelGGL((k_route_small<T, K, false>), dim3(1), dim3(kSmallThreads), lds, st, p);
+    const size_t lds = sizeof(int32_t) * (size_t)(p.n_experts + p.n * p.k);   // (n k <= 8 n, and n n_experts <= 32768: under 64 KB)
+    if (vec) hipLaunchKernelGGL((k_route_small<T, LANES, K, true>), dim3(1), dim3(kSmallThreads), lds, st, p);
+    else hipLaunchKernelGGL((k_route_small<T, LANES, K, false>), dim3(1), dim3(kSmallThreads), lds, st, p);
 }
 template <typename T, int K>
 void launch_route(const RouteArgs& p, bool vec, hipStream_t st) {
     if (is_small(p.n, p.n_experts)) {
-        launch_small<T, K>(p, vec, st);
+        // few rows: a wavefront each; more: four a wavefront, as long as a row is a few loads of 16 lanes
+        if (p.n <= kSmallThreads / 64 || p.n_experts > 512) launch_small<T, 64, K>(p, vec, st);
+        else launch_small<T, 16, K>(p, vec, st);
         return;
     }
     if (p.n_experts <= 512) launch_pick<T, 16, K>(p, vec, st);
     else launch_pick<T, 64, K>(p, vec, st);
     hipLaunchKernelGGL(k_route_scan, dim3(blocks_of(p.n_experts, kScanColumns)), dim3(kScanThreads), 0, st, p);
-    hipLaunchKernelGGL(k_route_place, dim3((uint32_t)p.n_chunks), dim3(64), sizeof(int32_t) * (size_t)p.n_experts, st, p);
+    if (p.n_experts <= 2048) hipLaunchKernelGGL(k_route_place<4>, dim3((uint32_t)p.n_chunks), dim3(256), sizeof(int32_t) * 4 * (size_t)p.n_experts, st, p);
+    else hipLaunchKernelGGL(k_route_place<1>, dim3((uint32_t)p.n_chunks), dim3(64), sizeof(int32_t) * (size_t)p.n_experts, st, p);
 }
 template <typename T>
 void launch_route_k(const RouteArgs& p, bool vec, hipStream_t st) {
@@ -51,17 +54,24 @@ void launch_route_k(const RouteArgs& p, bool vec, hipStream_t st) {
     else launch_route<T, 8>(p, vec, st);
 }
 
-template <typename T>
+template <typename T, int K>
 void launch_route_gradient(const RouteGradientArgs& p, bool vec, hipStream_t st) {
     if (p.n_experts <= 512) {
         const dim3 grid = grid_of((p.n + 15) / 16);
-        if (vec) hipLaunchKernelGGL((k_route_gradient<T, 16, true>), grid, dim3(256), 0, st, p);
-        else hipLaunchKernelGGL((k_route_gradient<T, 16, false>), grid, dim3(256), 0, st, p);
+        if (vec) hipLaunchKernelGGL((k_route_gradient<T, 16, K, true>), grid, dim3(256), 0, st, p);
+        else hipLaunchKernelGGL((k_route_gradient<T, 16, K, false>), grid, dim3(256), 0, st, p);
     } else {
         const dim3 grid = grid_of((p.n + 3) / 4);
-        if (vec) hipLaunchKernelGGL((k_route_gradient<T, 64, true>), grid, dim3(256), 0, st, p);
-        else hipLaunchKernelGGL((k_route_gradient<T, 64, false>), grid, dim3(256), 0, st, p);
+        if (vec) hipLaunchKernelGGL((k_route_gradient<T, 64, K, true>), grid, dim3(256), 0, st, p);
+        else hipLaunchKernelGGL((k_route_gradient<T, 64, K, false>), grid, dim3(256), 0, st, p);
     }
+}
+template <typename T>
+void launch_route_gradient_k(const RouteGradientArgs& p, bool vec, hipStream_t st) {
+    if (p.k == 1) launch_route_gradient<T, 1>(p, vec, st);
+    else if (p.k == 2) launch_route_gradient<T, 2>(p, vec, st);
+    else if (p.k <= 4) launch_route_gradient<T, 4>(p, vec, st);
+    else launch_route_gradient<T, 8>(p, vec, st);
 }
 
 template <typename T, int VEC, int LANES>
@@ -147,9 +157,9 @@ extern "C" int nomad_route_gradient(const void* logits, int32_t dtype, int64_t n
     const int64_t size = size_of(dtype);
     const bool vec = (normalize || by(logits, stride, size, 16)) && by(dlogits, n_experts, size, 16);
     hipStream_t st = (hipStream_t)stream;
-    if (dtype == NOMAD_F32) launch_route_gradient<float>(p, vec, st);
-    else if (dtype == NOMAD_BF16) launch_route_gradient<__bf16>(p, vec, st);
-    else launch_route_gradient<_Float16>(p, vec, st);
+    if (dtype == NOMAD_F32) launch_route_gradient_k<float>(p, vec, st);
+    else if (dtype == NOMAD_BF16) launch_route_gradient_k<__bf16>(p, vec, st);
+    else launch_route_gradient_k<_Float16>(p, vec, st);
     KTRY(hipGetLastError());
     return NOMAD_OK;
 }

@@ -6,7 +6,10 @@ current stream (or `stream`) and returns without waiting.  Gradients are calls o
 tape.  Arguments that do not fit raise ValueError before anything is enqueued."""
 from __future__ import annotations
 
+import array
 import ctypes as C
+import itertools
+import operator
 from typing import NamedTuple
 
 from . import binding
@@ -15,6 +18,14 @@ from .binding import NomadError, load_library
 MAX_K, MAX_EXPERTS, BLOCK = 8, 16384, 256
 ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3}
 _DTYPES = None
+
+
+_get_dtype = operator.attrgetter("dtype")
+
+
+def _is_tensor(t):
+    import torch
+    return isinstance(t, torch.Tensor)
 
 
 def _dtypes():
@@ -97,16 +108,16 @@ def route(logits, k, normalize=True, stream=None) -> Routing:
     if not 1 <= k <= min(MAX_K, experts) or experts > MAX_EXPERTS:
         raise ValueError(f"k = {k} of {experts} experts: 1 <= k <= {MAX_K} and no more than there are (at most {MAX_EXPERTS})")
     lib = load_library()
-    # one allocation: experts, weights, order and slots of n k words each, the offsets, the work space
-    words = n * k
     need = lib.nomad_route_workspace(n, experts, k)
-    held = torch.empty(4 * words + experts + 1 + need // 4, dtype=torch.int32, device=device)
-    parts = held.split_with_sizes([words, words, words, words, experts + 1, need // 4])
-    out = Routing(parts[0].view(n, k), parts[1].view(torch.float32).view(n, k), parts[4], parts[2], parts[3].view(n, k))
-    st = _stream(device, stream, (logits, held))
-    base = held.data_ptr()
-    _check(lib.nomad_route(logits.data_ptr(), code, n, stride, experts, k, 1 if normalize else 0, base, base + 4 * words, base + 16 * words, base + 8 * words,
-                           base + 12 * words, base + 4 * (4 * words + experts + 1), need, device.index, st or None), "nomad_route")
+    held = torch.empty((4, n, k), dtype=torch.int32, device=device)
+    chosen, weights, order, slots = held.unbind(0)
+    offsets = torch.empty(experts + 1, dtype=torch.int32, device=device)
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    out = Routing(chosen, weights.view(torch.float32), offsets, order.view(-1), slots)
+    st = _stream(device, stream, (logits, held, offsets, work))
+    base, words = held.data_ptr(), 4 * n * k
+    _check(lib.nomad_route(logits.data_ptr(), code, n, stride, experts, k, 1 if normalize else 0, base, base + words, offsets.data_ptr(), base + 2 * words,
+                           base + 3 * words, work.data_ptr() if need else None, need, device.index, st or None), "nomad_route")
     return out
 
 
@@ -311,38 +322,49 @@ def adamw_step(params, grads, first, second, step, lr=1e-3, betas=(0.9, 0.999), 
     _on(device, grad_scale=grad_scale)
     if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
         raise ValueError("grad_scale must be one float32 element")
-    codes = _dtypes()
-    table = (binding.AdamWTensor * len(params))()
-    used = [grad_scale]
-    for row, p, g, m, v in zip(table, params, grads, first, second):
-        n = p.numel()
-        if p.dtype not in codes or (g.dtype != p.dtype and g.dtype != torch.float32 and (p.dtype != torch.float32 or g.dtype not in codes)):
-            raise ValueError(f"no step for {p.dtype} with gradients in {g.dtype}")
-        if isinstance(m, torch.Tensor) == eight or isinstance(v, torch.Tensor) == eight:
+    # every check is a pass over all tensors by one C function: a step over a hundred small tensors takes the host longer than the GPU
+    tensors = params + grads
+    if eight:
+        if any(map(_is_tensor, first)) or any(map(_is_tensor, second)):
             raise ValueError("the states must all be in 32 bits, or all in 8")
-        if eight:
-            (m, ms), (v, vs) = m, v
-            blocks = -(-n // BLOCK)
-            if m.dtype != torch.int8 or v.dtype != torch.uint8 or ms.dtype != torch.float32 or vs.dtype != torch.float32 or ms.numel() != blocks or vs.numel() != blocks:
-                raise ValueError(f"8-bit states of {n} elements: int8 and uint8 codes and {blocks} float32 scales each")
-            more = (ms, vs)
-            row.m_scale, row.v_scale = ms.data_ptr(), vs.data_ptr()
-        else:
-            if m.dtype != torch.float32 or v.dtype != torch.float32:
-                raise ValueError("32-bit states are float32")
-            more = ()
-        if g.numel() != n or m.numel() != n or v.numel() != n:
-            raise ValueError("a tensor, its gradient and its states must have as many elements")
-        for t in (p, g, m, v) + more:
-            if t.device != device or not t.is_contiguous():
-                raise ValueError(f"tensors must be contiguous and on {device}")
-        row.p, row.g, row.m, row.v, row.n, row.p_dtype, row.g_dtype = p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), n, codes[p.dtype], codes[g.dtype]
-        if stream is not None:
-            used.extend((p, g, m, v) + more)
-    st = _stream(device, stream, used)
+        m, m_scale = [s[0] for s in first], [s[1] for s in first]
+        v, v_scale = [s[0] for s in second], [s[1] for s in second]
+        tensors += m + v + m_scale + v_scale
+        wanted = ((m, {torch.int8}), (v, {torch.uint8}), (m_scale, {torch.float32}), (v_scale, {torch.float32}))
+    else:
+        if not (all(map(_is_tensor, first)) and all(map(_is_tensor, second))):
+            raise ValueError("the states must all be in 32 bits, or all in 8")
+        m, v = first, second
+        tensors += m + v
+        wanted = ((m, {torch.float32}), (v, {torch.float32}))
+    if set(map(torch.Tensor.get_device, tensors)) != {device.index} or not all(map(torch.Tensor.is_contiguous, tensors)):
+        raise ValueError(f"tensors must be contiguous and on {device}")
+    for which, dtypes in wanted:
+        if set(map(_get_dtype, which)) != dtypes:
+            raise ValueError("states are float32 in 32 bits; int8 and uint8 codes with float32 scales in 8")
+    sizes = list(map(torch.Tensor.numel, params))
+    if any(list(map(torch.Tensor.numel, which)) != sizes for which in (grads, m, v)):
+        raise ValueError("a tensor, its gradient and its states must have as many elements")
+    if eight:
+        blocks = [-(-n // BLOCK) for n in sizes]
+        if any(list(map(torch.Tensor.numel, which)) != blocks for which in (m_scale, v_scale)):
+            raise ValueError(f"8-bit states have a scale for every {BLOCK} elements")
+    codes = _dtypes()
+    kinds = list(zip(map(_get_dtype, params), map(_get_dtype, grads)))
+    for p, g in set(kinds):
+        if p not in codes or g not in codes or (g != p and torch.float32 not in (p, g)):
+            raise ValueError(f"no step for {p} with gradients in {g}")
+    count, pointer = len(params), torch.Tensor.data_ptr
+    none = [0] * count
+    words = {k: codes[k[0]] | codes[k[1]] << 32 for k in set(kinds)}   # (p_dtype and g_dtype, two 32-bit fields)
+    rows = zip(map(pointer, params), map(pointer, grads), map(pointer, m), map(pointer, v), map(pointer, m_scale) if eight else none,
+               map(pointer, v_scale) if eight else none, sizes, map(words.__getitem__, kinds))
+    flat = array.array("q", itertools.chain.from_iterable(rows))
+    table = (binding.AdamWTensor * count).from_buffer(flat)
+    st = _stream(device, stream, tensors + [grad_scale])
     options = binding.AdamWOptions(C.sizeof(binding.AdamWOptions), 8 if eight else 32, int(step), float(lr), float(betas[0]), float(betas[1]), float(eps),
                                    float(weight_decay), grad_scale.data_ptr() if grad_scale is not None else None, st or None, device.index)
-    _check(load_library().nomad_adamw_step(table, len(params), C.byref(options)), "nomad_adamw_step")
+    _check(load_library().nomad_adamw_step(table, count, C.byref(options)), "nomad_adamw_step")
 
 
 def adamw_state_values(states, stream=None):

@@ -19,23 +19,29 @@ int main() {
         const GradientPlan p = plan_gradient(r, g, in, out, small, 256);
         if (p.most < 256 || p.tiles < 1) return 1;
         if ((p.slots > 0) != (r > p.most)) return 2;
-        // every part of a long group begins in a slot of its own, and the slots are there: groups of every length, one after the other
-        if (p.slots > 0 && (r - 1) / (p.most / 2) >= p.slots) return 3;
+        // every row's slot is there, and a slot has no more rows than half of the longest part
+        if (p.slots > 0 && (r - 1) >> p.slot_bits >= p.slots) return 3;
+        if ((int64_t)1 << p.slot_bits > p.most / 2) return 8;
         if (!small && p.tile == kGradient256) return 4;
-        const ProductTile t = plan_product(r, g, in, out, small, 256);
-        if ((out <= 16) != (t == kProduct16) || (!small && t == kProduct256)) return 5;
+        for (int w_kc = 0; w_kc < 2; ++w_kc) {
+            const ProductTile t = plan_product(r, g, out, small, w_kc, 256);
+            if ((!small && t == kProduct256) || (!w_kc && t == kProductFew)) return 5;
+            if (out <= 16 && t != kProduct16 && t != kProductFew) return 9;
+        }
     }
-    // parts of a group of n rows, as the kernels cut them
+    // parts of a group of n rows, as the kernels cut them: each in a slot of its own, and so is the next group's first
     for (int64_t most : {256, 257, 1001, 4687})
         for (int64_t n : {most + 1, 2 * most, 2 * most + 1, 10 * most + 3, 1000 * most - 1}) {
-            const int64_t parts = (n + most - 1) / most;
+            const int64_t parts = (n + most - 1) / most, each = n / parts, left = n % parts;
+            int bits = 0;
+            while ((int64_t)2 << bits <= most / 2) ++bits;
             int64_t before = -1;
             for (int64_t j = 0; j < parts; ++j) {
-                const int64_t begin = 77 + n * j / parts, end = 77 + n * (j + 1) / parts, slot = begin / (most / 2);
-                if (end - begin > most || end - begin < most / 2 || slot == before) return 6;
+                const int64_t begin = 77 + j * each + (j < left ? j : left), end = 77 + (j + 1) * each + (j + 1 < left ? j + 1 : left), slot = begin >> bits;
+                if (end - begin > most || end - begin < most / 2 || slot == before || (j + 1 == parts && end != 77 + n)) return 6;
                 before = slot;
             }
-            if ((77 + n) / (most / 2) == before) return 7;    // the next group's first part
+            if ((77 + n) >> bits == before) return 7;
         }
     std::puts("ok");
     return 0;
