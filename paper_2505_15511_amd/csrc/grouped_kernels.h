@@ -212,7 +212,7 @@ struct Source {
 };
 
 // TILE rows (KC) or columns (not KC) by one stage of k, for NT threads.  PICKED: source rows anywhere (KC: a pointer each; otherwise
-// their numbers are read a stage ahead).  ASYNC: loads go to LDS directly, whole 16-byte chunks; otherwise through registers, element by element where a chunk is cut off.
+// the numbers of 64 rows at a time in a register of the wavefront, the next 64 on their way).  ASYNC: loads go to LDS directly, whole 16-byte chunks; otherwise through registers, element by element where a chunk is cut off.
 template <typename T, int TILE, bool KC, bool PICKED, int Q, bool ASYNC, int NT>
 struct Operand {
     static constexpr int kEpc = 16 / (int)sizeof(T);             // elements a chunk
@@ -226,7 +226,7 @@ struct Operand {
     Source src;
     int64_t first;                 // not KC: the place of k = 0
     int32_t across;                // not KC: columns before the tile
-    int32_t place[!KC && PICKED ? kPer : 1];   // not KC, picked: entries of the order for the next stage's rows
+    int32_t now, next;             // not KC, picked: source rows of 64 places (-1: none), entries of the order of the 64 behind them
     int32_t limit;                 // k there are (KC: of every row)
     int32_t width;                 // not KC: columns there are, from the tile's first
     uint4 held[ASYNC ? 1 : kPer];
@@ -260,16 +260,10 @@ struct Operand {
         limit = k_limit;
         across = column;
         width = columns - column;
-        if (PICKED) fetch(0, tid);
+        if (PICKED) next = entry(tid & 63);
         else row[0] = (const T*)s.base + (first_k + tid / kCpr) * s.stride + column;
     }
-    __device__ __forceinline__ void fetch(int32_t k0, int tid) {
-#pragma unroll
-        for (int it = 0; it < kPer; ++it) {
-            const int32_t k = k0 + (it * NT + tid) / kCpr;
-            place[!KC && PICKED ? it : 0] = k >= limit ? -1 : src.order ? src.order[first + k] : (int32_t)(first + k);
-        }
-    }
+    __device__ __forceinline__ int32_t entry(int32_t k) const { return k >= limit ? -1 : src.order ? src.order[first + k] : (int32_t)(first + k); }
     __device__ __forceinline__ void chunk(int it, int tid, int32_t k0, const T*& from, int& elements) const {
         const int l = it * NT + tid, r = l / kCpr, c = (l % kCpr) ^ chunk_twist<T, TILE, KC, Q>(r);
         if (KC) {
@@ -281,7 +275,7 @@ struct Operand {
             const int32_t k = k0 + r;
             int64_t at = 0;
             if (PICKED) {
-                at = src.row_at(place[!KC && PICKED ? it : 0]);
+                at = __shfl(now, k & 63);
                 from = (const T*)src.base + at * src.stride + across + c * kEpc;
             } else {
                 constexpr int apart = NT / kCpr;
@@ -290,8 +284,12 @@ struct Operand {
             elements = k < limit && at >= 0 ? width - c * kEpc : 0;
         }
     }
-    // asks for the stage that begins at k0
+    // asks for the stage that begins at k0 (stages in their order)
     __device__ __forceinline__ void ask(uint4* lds, int32_t k0, int tid) {
+        if (!KC && PICKED && (k0 & 63) == 0) {
+            now = (int32_t)src.row_at(next);
+            next = entry(k0 + 64 + (tid & 63));
+        }
 #pragma unroll
         for (int it = 0; it < kPer; ++it) {
             if (!has(it, tid)) continue;   // (kChunks is a multiple of 64: whole wavefronts)
@@ -316,7 +314,6 @@ struct Operand {
                 held[ASYNC ? 0 : it] = v;
             }
         }
-        if (!KC && PICKED) fetch(k0 + kBk, tid);
     }
     // puts down what was asked for, where the loads did not
     __device__ __forceinline__ void put(uint4* lds, int tid) const {
@@ -389,13 +386,14 @@ struct Tile {
         if (ASYNC) __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
         __syncthreads();
     }
-    // acc += sum over k < limit, the first stage having been asked for.  Behind it all four stages are free.  SUMS, where with_sums:
-    // also the sums of B alone over k; the wavefronts side by side along a share their columns, kSums fragments each.
+    // acc += sum over k < limit, the first stage having been asked for.  Behind it all four stages are free.  SUMS: also the
+    // sums of B alone over k; the wavefronts side by side along a share their columns, kSums fragments each.
     static constexpr int kSums = kFb < WA ? 1 : kFb / WA;
     static __device__ __forceinline__ bool sums_of(int y, int tid) { return y / kSums == (tid >> 6) % WA; }
     template <bool SUMS>
-    __device__ __forceinline__ void run(A& a, B& b, uint4* a0, uint4* b0, uint4* a1, uint4* b1, int32_t limit, f32x4* sums, bool with_sums, int tid) {
+    __device__ __forceinline__ void run(A& a, B& b, uint4* a0, uint4* b0, uint4* a1, uint4* b1, int32_t limit, f32x4* sums, int tid) {
         const int lane = tid & 63, wave = tid >> 6, wa = (wave % WA) * (TA / WA), wb = (wave / WA) * (TB / WB);
+        const int ws = wb + (wave % WA * kSums < kFb ? wave % WA * kSums * 16 : 0);   // (read once more: choosing among the fragments at hand would be a branch)
         const auto step = [&](const uint4* la, const uint4* lb) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
@@ -408,10 +406,20 @@ struct Tile {
                 for (int y = 0; y < kFb; ++y)
 #pragma unroll
                     for (int x = 0; x < kFa; ++x) acc[x][y] = Elem<T>::mma(fa[x], fb[y], acc[x][y]);
-                if (SUMS && with_sums)
+                if (SUMS)
 #pragma unroll
-                    for (int y = 0; y < kFb; ++y)
-                        if (y / kSums == wave % WA) sums[y % kSums] = Elem<T>::mma(Elem<T>::ones(), fb[y], sums[y % kSums]);
+                    for (int q = 0; q < kSums; ++q) sums[q] = Elem<T>::mma(Elem<T>::ones(), B::fragment(lb, ws, q, s, lane), sums[q]);
+            }
+            if constexpr (!A_KC && B_KC && sizeof(T) == 2 && kFb > 1) {
+                // the order of the stage's instructions: what the first products need, then reads between products, two of B's fragments
+                // ahead (left to itself the compiler reads all of a step, waits for it, and multiplies: LDS and matrix cores take turns)
+                constexpr int ra = kFa * (A_KC ? 1 : 2), rb = (B_KC ? 1 : 2), reads = 2 * (ra + kFb * rb), ahead = ra + 2 * rb, slots = kFb > 1 ? 2 * kFb - 2 : 1;
+                __builtin_amdgcn_sched_group_barrier(0x100, ahead, 0);
+#pragma unroll
+                for (int i = 0; i < 2 * kFb; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, kFa, 0);
+                    if (i < slots) __builtin_amdgcn_sched_group_barrier(0x100, (reads - ahead + slots - 1) / slots, 0);
+                }
             }
         };
         if (limit <= 0) return;
@@ -525,18 +533,28 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_product(ProductArgs
     for (bool have = false;; have = true) {
         if (have) {
             // the sums begin with the bias
+            float start[Work::kSets][N] = {};
+            if (p.bias && group < p.n_groups) {
+                const T* from = (const T*)p.bias + (int64_t)group * p.bias_stride + column;
 #pragma unroll
-            for (int set = 0; set < Work::kSets; ++set) {
-                const int32_t col = column + Work::column(set, tid);
-                const T* from = (const T*)p.bias + (int64_t)group * p.bias_stride + col;
+                for (int set = 0; set < Work::kSets; ++set) {
+                    const int32_t col = Work::column(set, tid), n = p.out - column - col;
+                    T some[N] = {};
+                    if (n >= N) __builtin_memcpy(some, from + col, sizeof(some));   // (aligned as an element is)
+                    else if (n > 0)
+                        for (int j = 0; j < N; ++j)
+                            if (j < n) some[j] = from[col + j];
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const float start = p.bias && group < p.n_groups && (STORES ? col : col + j) < p.out ? (float)from[j] : 0.f;
-#pragma unroll
-                    for (int y = 0; y < Work::kFb; ++y) work.at(set, y, j) = start;
+                    for (int j = 0; j < N; ++j) start[set][j] = (float)some[j];
                 }
             }
-            work.template run<false>(a, b, a0, b0, a1, b1, group < p.n_groups ? p.in : 0, nullptr, false, tid);
+#pragma unroll
+            for (int set = 0; set < Work::kSets; ++set)
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+#pragma unroll
+                    for (int y = 0; y < Work::kFb; ++y) work.at(set, y, j) = start[set][j];
+            work.template run<false>(a, b, a0, b0, a1, b1, group < p.n_groups ? p.in : 0, nullptr, tid);
         }
         const int32_t done_group = group, done_column = column, done_count = count;
         const int64_t done_first = first;
@@ -782,7 +800,8 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_gradient(GradientAr
             work.clear();
 #pragma unroll
             for (int y = 0; y < Work::kSums; ++y) sums[y] = f32x4{0.f, 0.f, 0.f, 0.f};
-            work.template run<true>(a, b, a0, b0, a1, b1, unit.count, sums, bias, tid);
+            if (bias) work.template run<true>(a, b, a0, b0, a1, b1, unit.count, sums, tid);
+            else work.template run<false>(a, b, a0, b0, a1, b1, unit.count, sums, tid);
         }
         const Unit done = unit;
         const int32_t done_a = a_first, done_b = b_first;
