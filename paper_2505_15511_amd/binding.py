@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -46,34 +47,12 @@ TUNE = {"edge_block": 1, "workgroups_per_cu": 2, "scatter_path": 3, "pool_kernel
 POOL_PICKS16, POOL_DISTINCT, POOL_STRATIFIED = 0, 1, 2
 
 
-class GroupedProductArgs(C.Structure):
-    """nomad_grouped_product_args"""
-    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("out_dtype", C.c_int32), ("activation", C.c_int32), ("n_groups", C.c_int32),
-                ("per_row", C.c_int32), ("in_", C.c_int32), ("out", C.c_int32), ("rows", C.c_int64), ("x_rows", C.c_int64), ("offsets", C.c_void_p),
-                ("order", C.c_void_p), ("x", C.c_void_p), ("x_stride", C.c_int64), ("w", C.c_void_p), ("w_group_stride", C.c_int64),
-                ("w_out_stride", C.c_int64), ("w_in_stride", C.c_int64), ("bias", C.c_void_p), ("bias_stride", C.c_int64), ("slope_at", C.c_void_p),
-                ("slope_stride", C.c_int64), ("y", C.c_void_p), ("y_stride", C.c_int64), ("z_out", C.c_void_p), ("z_stride", C.c_int64),
-                ("stream", C.c_void_p), ("device", C.c_int32)]
-
-
-class GroupedGradientArgs(C.Structure):
-    """nomad_grouped_gradient_args"""
-    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("out_dtype", C.c_int32), ("n_groups", C.c_int32), ("per_row", C.c_int32),
-                ("in_", C.c_int32), ("out", C.c_int32), ("rows", C.c_int64), ("x_rows", C.c_int64), ("offsets", C.c_void_p), ("order", C.c_void_p),
-                ("dy", C.c_void_p), ("dy_stride", C.c_int64), ("x", C.c_void_p), ("x_stride", C.c_int64), ("dw", C.c_void_p), ("db", C.c_void_p),
-                ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64), ("stream", C.c_void_p), ("device", C.c_int32)]
-
-
-class AdamWTensor(C.Structure):
-    """nomad_adamw_tensor"""
-    _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p), ("v_scale", C.c_void_p),
-                ("n", C.c_int64), ("p_dtype", C.c_int32), ("g_dtype", C.c_int32)]
-
-
-class AdamWOptions(C.Structure):
-    """nomad_adamw_options"""
-    _fields_ = [("struct_size", C.c_uint32), ("bits", C.c_int32), ("step", C.c_int64), ("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double),
-                ("eps", C.c_double), ("weight_decay", C.c_double), ("grad_scale", C.c_void_p), ("stream", C.c_void_p), ("device", C.c_int32)]
+# Layouts of the argument structures of the learned map's operators, in the order of their fields (include/nomad.h); packing one takes a
+# fraction of the time that filling a ctypes.Structure does, and a call on a few rows is mostly that.
+GROUPED_PRODUCT_ARGS = struct.Struct("@I7i2q3Pq" "P3q" "PqPqPqPq" "Pi4x")
+GROUPED_GRADIENT_ARGS = struct.Struct("@I6i4x2q2P" "PqPq" "PP" "Pq" "Pi4x")
+ADAMW_TENSOR = struct.Struct("@6Pq2i")
+ADAMW_OPTIONS = struct.Struct("@Iiq5dPPi4x")
 
 
 class NomadError(RuntimeError):
@@ -135,13 +114,13 @@ def load_library():
     lib.nomad_route_workspace.restype = i64
     lib.nomad_route.argtypes = [vp, i32, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, i64, i32, vp]
     lib.nomad_route_gradient.argtypes = [vp, i32, i64, i64, i32, i32, i32, vp, vp, vp, vp, i32, vp]
-    lib.nomad_grouped_product.argtypes = [C.POINTER(GroupedProductArgs)]
+    lib.nomad_grouped_product.argtypes = [vp]
     lib.nomad_grouped_gradient_workspace.argtypes = [i64, i32, i32, i32, i32]
     lib.nomad_grouped_gradient_workspace.restype = i64
-    lib.nomad_grouped_weight_gradient.argtypes = [C.POINTER(GroupedGradientArgs)]
+    lib.nomad_grouped_weight_gradient.argtypes = [vp]
     lib.nomad_combine.argtypes = [vp, i32, i64, i64, i32, vp, vp, i64, i32, vp, i32, vp]
     lib.nomad_combine_gradient.argtypes = [vp, i32, i64, vp, i64, i64, i32, vp, vp, vp, i64, i32, vp, vp, i32, vp]
-    lib.nomad_adamw_step.argtypes = [C.POINTER(AdamWTensor), i32, C.POINTER(AdamWOptions)]
+    lib.nomad_adamw_step.argtypes = [vp, i32, vp]
     lib.nomad_adamw_state_values.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp]
     lib.nomad_last_error.argtypes = [vp]
     lib.nomad_last_error.restype = C.c_char_p

@@ -12,65 +12,58 @@ import itertools
 import operator
 from typing import NamedTuple
 
+import torch
+
 from . import binding
 from .binding import NomadError, load_library
 
 MAX_K, MAX_EXPERTS, BLOCK = 8, 16384, 256
 ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3}
-_DTYPES = None
-
-
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _get_dtype = operator.attrgetter("dtype")
 
 
-def _is_tensor(t):
-    import torch
-    return isinstance(t, torch.Tensor)
-
-
-def _dtypes():
-    global _DTYPES
-    if _DTYPES is None:
-        import torch
-        _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-    return _DTYPES
+def _all_tensors(things):
+    return all(issubclass(kind, torch.Tensor) for kind in set(map(type, things)))
 
 
 def _dtype(t, name):
-    code = _dtypes().get(t.dtype)
+    code = _DTYPES.get(t.dtype)
     if code is None:
         raise ValueError(f"{name} must be float32, bfloat16 or float16, not {t.dtype}")
     return code
 
 
-def _on(device, **tensors):
+def _on(device, *tensors):
     """The tensors that are not None live on `device` (a torch.device of a GPU)."""
     if device.type != "cuda":
         raise ValueError("the operators take tensors on the GPU")
-    for name, t in tensors.items():
+    for t in tensors:
         if t is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, not on {device}")
+            raise ValueError(f"a tensor is on {t.device}, another one on {device}")
 
 
 def _whole(t, name, dtype, shape):
     """`t` is contiguous, of that type and shape."""
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
 
 
 def _rows(t, name, columns=None):
-    """(rows, stride) of a matrix whose columns are contiguous."""
-    if t.dim() != 2 or (columns is not None and t.shape[1] != columns):
-        raise ValueError(f"{name} must be a matrix" + (f" of {columns} columns" if columns is not None else "") + f", got shape {tuple(t.shape)}")
-    if t.shape[1] > 1 and t.stride(1) != 1 and t.numel():
+    """(rows, columns, stride) of a matrix whose columns are contiguous."""
+    shape = t.shape
+    if len(shape) != 2 or (columns is not None and shape[1] != columns):
+        raise ValueError(f"{name} must be a matrix" + (f" of {columns} columns" if columns is not None else "") + f", got shape {tuple(shape)}")
+    rows, columns = shape
+    apart, beside = t.stride()
+    if beside != 1 and columns > 1 and rows:
         raise ValueError(f"the columns of {name} must be contiguous (strides {t.stride()})")
-    return t.shape[0], (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    return rows, columns, apart if rows > 1 else columns
 
 
 def _stream(device, stream, used):
     """The stream of a call.  What it uses of torch's memory is not handed out again before a stream other than the current one
     has come by here."""
-    import torch
     chosen = binding._call_stream(device.index, stream)
     if stream is not None and chosen != torch._C._cuda_getCurrentRawStream(device.index):
         other = torch.cuda.ExternalStream(int(chosen), device=device)
@@ -98,62 +91,56 @@ class Routing(NamedTuple):
 def route(logits, k, normalize=True, stream=None) -> Routing:
     """nomad_route: the k experts with the largest logits of every row [n, n_experts], their weights, and the rows in the order
     of their experts."""
-    import torch
     device = logits.device
     _on(device)
     code = _dtype(logits, "logits")
-    n, stride = _rows(logits, "logits")
-    experts = logits.shape[1]
+    n, experts, stride = _rows(logits, "logits")
     k = int(k)
     if not 1 <= k <= min(MAX_K, experts) or experts > MAX_EXPERTS:
         raise ValueError(f"k = {k} of {experts} experts: 1 <= k <= {MAX_K} and no more than there are (at most {MAX_EXPERTS})")
     lib = load_library()
     need = lib.nomad_route_workspace(n, experts, k)
-    held = torch.empty((4, n, k), dtype=torch.int32, device=device)
-    chosen, weights, order, slots = held.unbind(0)
+    chosen, slots = torch.empty(n, k, dtype=torch.int32, device=device), torch.empty(n, k, dtype=torch.int32, device=device)
+    weights, order = torch.empty(n, k, dtype=torch.float32, device=device), torch.empty(n * k, dtype=torch.int32, device=device)
     offsets = torch.empty(experts + 1, dtype=torch.int32, device=device)
     work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    out = Routing(chosen, weights.view(torch.float32), offsets, order.view(-1), slots)
-    st = _stream(device, stream, (logits, held, offsets, work))
-    base, words = held.data_ptr(), 4 * n * k
-    _check(lib.nomad_route(logits.data_ptr(), code, n, stride, experts, k, 1 if normalize else 0, base, base + words, offsets.data_ptr(), base + 2 * words,
-                           base + 3 * words, work.data_ptr() if need else None, need, device.index, st or None), "nomad_route")
+    st = _stream(device, stream, (logits, chosen, weights, offsets, order, slots, work))
+    _check(lib.nomad_route(logits.data_ptr(), code, n, stride, experts, k, 1 if normalize else 0, chosen.data_ptr(), weights.data_ptr(), offsets.data_ptr(),
+                           order.data_ptr(), slots.data_ptr(), work.data_ptr() if need else None, need, device.index, st or None), "nomad_route")
+    out = Routing(chosen, weights, offsets, order, slots)
     return out
 
 
 def route_gradient(logits, routing, dweights, normalize=True, stream=None):
     """nomad_route_gradient: the gradient of the logits from that of the weights; normalize as in the call of `route`."""
-    import torch
     device = logits.device
-    _on(device, experts=routing.experts, weights=routing.weights, dweights=dweights)
+    _on(device, routing.experts, routing.weights, dweights)
     code = _dtype(logits, "logits")
-    n, stride = _rows(logits, "logits")
+    n, experts, stride = _rows(logits, "logits")
     k = routing.experts.shape[1]
     _whole(routing.experts, "routing.experts", torch.int32, (n, k))
     _whole(routing.weights, "routing.weights", torch.float32, (n, k))
     _whole(dweights, "dweights", torch.float32, (n, k))
-    out = torch.empty(n, logits.shape[1], dtype=logits.dtype, device=device)
+    out = torch.empty(n, experts, dtype=logits.dtype, device=device)
     st = _stream(device, stream, (logits, routing.experts, routing.weights, dweights, out))
-    _check(load_library().nomad_route_gradient(logits.data_ptr(), code, n, stride, logits.shape[1], k, 1 if normalize else 0, routing.experts.data_ptr(),
+    _check(load_library().nomad_route_gradient(logits.data_ptr(), code, n, stride, experts, k, 1 if normalize else 0, routing.experts.data_ptr(),
                                                routing.weights.data_ptr(), dweights.data_ptr(), out.data_ptr(), device.index, st or None), "nomad_route_gradient")
     return out
 
 
-def _grouping(x, offsets, order, per_row, rows):
+def _grouping(x_rows, offsets, order, per_row, rows):
     """Checks of what says which row of x stands at which place; the number of places."""
-    import torch
-    if offsets.dtype != torch.int32 or offsets.dim() != 1 or not offsets.is_contiguous() or offsets.numel() < 2:
+    if offsets.dtype != torch.int32 or offsets.dim() != 1 or not offsets.is_contiguous() or offsets.shape[0] < 2:
         raise ValueError("offsets must be a contiguous int32 tensor of one entry more than there are groups")
+    places = x_rows
     if order is not None:
         if order.dtype != torch.int32 or order.dim() != 1 or not order.is_contiguous():
             raise ValueError("order must be a contiguous int32 tensor")
         if int(per_row) < 1:
             raise ValueError("per_row must be at least 1")
-        places = order.numel()
-        if places and not x.shape[0]:
+        places = order.shape[0]
+        if places and not x_rows:
             raise ValueError("order asks for rows of an empty x")
-    else:
-        places = x.shape[0]
     if rows is not None and rows != places:
         raise ValueError(f"{places} places, but {rows} rows")
     return places
@@ -163,19 +150,19 @@ def grouped_product(x, w, offsets, bias=None, activation=None, order=None, per_r
     """nomad_grouped_product: y_p = act(x_p W_e^T + b_e) for the places p of every group e (offsets [E + 1]), x_p = x[p] or
     x[order[p] // per_row].  w [E, out, in] in either order of its last two strides; keep=True returns (y, z) with z the products
     before the activation; slope_at=z multiplies by the activation's slope at z instead (the way back)."""
-    import torch
     device = x.device
-    _on(device, w=w, offsets=offsets, bias=bias, order=order, slope_at=slope_at)
+    _on(device, w, offsets, bias, order, slope_at)
     code = _dtype(x, "x")
     if activation not in ACTIVATIONS:
         raise ValueError(f"activation must be one of {sorted(k for k in ACTIVATIONS if k)}")
-    if w.dim() != 3 or w.dtype != x.dtype or x.dim() != 2 or w.shape[2] != x.shape[1] or min(w.shape) < 1:
-        raise ValueError(f"w must be [experts, out, {x.shape[-1]}] of {x.dtype}, got {tuple(w.shape)} of {w.dtype}")
-    groups, out, inner = w.shape
-    x_rows, x_stride = _rows(x, "x")
-    places = _grouping(x, offsets, order, per_row, None)
-    if offsets.numel() != groups + 1:
-        raise ValueError(f"{groups} groups need {groups + 1} offsets, got {offsets.numel()}")
+    x_rows, columns, x_stride = _rows(x, "x")
+    shape = w.shape
+    if len(shape) != 3 or w.dtype != x.dtype or shape[2] != columns or 0 in shape:
+        raise ValueError(f"w must be [experts, out, {columns}] of {x.dtype}, got {tuple(shape)} of {w.dtype}")
+    groups, out, inner = shape
+    places = _grouping(x_rows, offsets, order, per_row, None)
+    if offsets.shape[0] != groups + 1:
+        raise ValueError(f"{groups} groups need {groups + 1} offsets, got {offsets.shape[0]}")
     sg, so, si = w.stride()
     if inner == 1:
         si = 1
@@ -192,35 +179,34 @@ def grouped_product(x, w, offsets, bias=None, activation=None, order=None, per_r
             raise ValueError("slope_at goes without bias and keep")
         if slope_at.dtype != x.dtype or slope_at.shape[0] != places:
             raise ValueError(f"slope_at must be [{places}, {out}] of {x.dtype}")
-        _, z_stride = _rows(slope_at, "slope_at", out)
+        _, _, z_stride = _rows(slope_at, "slope_at", out)
     out_dtype = x.dtype if out_dtype is None else out_dtype
     if out_dtype not in (x.dtype, torch.float32):
         raise ValueError("out_dtype must be x's type or float32")
     y = torch.empty(places, out, dtype=out_dtype, device=device)
     z = torch.empty(places, out, dtype=x.dtype, device=device) if keep else None
     st = _stream(device, stream, (x, w, offsets, bias, order, slope_at, y, z))
-    a = binding.GroupedProductArgs(
-        C.sizeof(binding.GroupedProductArgs), code, _dtypes()[out_dtype], ACTIVATIONS[activation], groups, int(per_row), inner, out, places, x_rows,
-        offsets.data_ptr(), order.data_ptr() if order is not None else None, x.data_ptr(), x_stride, w.data_ptr(), sg if groups > 1 else 0, so, si,
-        bias.data_ptr() if bias is not None else None, (bias.stride(0) if groups > 1 else 0) if bias is not None else 0,
-        slope_at.data_ptr() if slope_at is not None else None, z_stride, y.data_ptr(), out, z.data_ptr() if keep else None, out, st or None, device.index)
-    _check(load_library().nomad_grouped_product(C.byref(a)), "nomad_grouped_product")
+    a = binding.GROUPED_PRODUCT_ARGS.pack(
+        binding.GROUPED_PRODUCT_ARGS.size, code, _DTYPES[out_dtype], ACTIVATIONS[activation], groups, int(per_row), inner, out, places, x_rows,
+        offsets.data_ptr(), order.data_ptr() if order is not None else 0, x.data_ptr(), x_stride, w.data_ptr(), sg if groups > 1 else 0, so, si,
+        bias.data_ptr() if bias is not None else 0, bias.stride(0) if bias is not None and groups > 1 else 0,
+        slope_at.data_ptr() if slope_at is not None else 0, z_stride, y.data_ptr(), out, z.data_ptr() if keep else 0, out, st, device.index)
+    _check(load_library().nomad_grouped_product(a), "nomad_grouped_product")
     return (y, z) if keep else y
 
 
 def grouped_weight_gradient(dy, x, offsets, order=None, per_row=1, bias=True, out_dtype=None, stream=None):
     """nomad_grouped_weight_gradient: (dW [E, out, in], db [E, out] float32 or None) from dy [places, out] and the x, offsets and
     order of the product."""
-    import torch
     device = x.device
-    _on(device, dy=dy, offsets=offsets, order=order)
+    _on(device, dy, offsets, order)
     code = _dtype(x, "x")
     if dy.dtype != x.dtype:
         raise ValueError(f"dy is {dy.dtype}, x {x.dtype}")
-    x_rows, x_stride = _rows(x, "x")
-    rows, dy_stride = _rows(dy, "dy")
-    _grouping(x, offsets, order, per_row, rows)
-    groups, inner, out = offsets.numel() - 1, x.shape[1], dy.shape[1]
+    x_rows, inner, x_stride = _rows(x, "x")
+    rows, out, dy_stride = _rows(dy, "dy")
+    _grouping(x_rows, offsets, order, per_row, rows)
+    groups = offsets.shape[0] - 1
     if inner < 1 or out < 1:
         raise ValueError("x and dy need columns")
     out_dtype = x.dtype if out_dtype is None else out_dtype
@@ -232,28 +218,27 @@ def grouped_weight_gradient(dy, x, offsets, order=None, per_row=1, bias=True, ou
     need = lib.nomad_grouped_gradient_workspace(rows, groups, inner, out, code)
     work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
     st = _stream(device, stream, (x, dy, offsets, order, dw, db, work))
-    a = binding.GroupedGradientArgs(
-        C.sizeof(binding.GroupedGradientArgs), code, _dtypes()[out_dtype], groups, int(per_row), inner, out, rows, x_rows, offsets.data_ptr(),
-        order.data_ptr() if order is not None else None, dy.data_ptr(), dy_stride, x.data_ptr(), x_stride, dw.data_ptr(), db.data_ptr() if bias else None,
-        work.data_ptr() if need else None, need, st or None, device.index)
-    _check(lib.nomad_grouped_weight_gradient(C.byref(a)), "nomad_grouped_weight_gradient")
+    a = binding.GROUPED_GRADIENT_ARGS.pack(
+        binding.GROUPED_GRADIENT_ARGS.size, code, _DTYPES[out_dtype], groups, int(per_row), inner, out, rows, x_rows, offsets.data_ptr(),
+        order.data_ptr() if order is not None else 0, dy.data_ptr(), dy_stride, x.data_ptr(), x_stride, dw.data_ptr(), db.data_ptr() if bias else 0,
+        work.data_ptr() if need else 0, need, st, device.index)
+    _check(lib.nomad_grouped_weight_gradient(a), "nomad_grouped_weight_gradient")
     return dw, db
 
 
 def combine(values, slots, weights=None, stream=None):
     """nomad_combine: y_i = sum_j weights[i, j] values[slots[i, j]] (weights None: ones)."""
-    import torch
     device = values.device
-    _on(device, slots=slots, weights=weights)
+    _on(device, slots, weights)
     code = _dtype(values, "values")
-    n_values, stride = _rows(values, "values")
+    n_values, d, stride = _rows(values, "values")
     n, k = slots.shape
     _whole(slots, "slots", torch.int32, (n, k))
     if weights is not None:
         _whole(weights, "weights", torch.float32, (n, k))
-    y = torch.empty(n, values.shape[1], dtype=values.dtype, device=device)
+    y = torch.empty(n, d, dtype=values.dtype, device=device)
     st = _stream(device, stream, (values, slots, weights, y))
-    _check(load_library().nomad_combine(values.data_ptr(), code, n_values, stride, values.shape[1], slots.data_ptr(),
+    _check(load_library().nomad_combine(values.data_ptr(), code, n_values, stride, d, slots.data_ptr(),
                                         weights.data_ptr() if weights is not None else None, n, k, y.data_ptr(), device.index, st or None), "nomad_combine")
     return y
 
@@ -261,12 +246,10 @@ def combine(values, slots, weights=None, stream=None):
 def combine_gradient(dy, values, slots, weights=None, order=None, need_dvalues=True, need_dweights=True, stream=None):
     """nomad_combine_gradient: (dvalues like values, dweights [n, k] float32); what is not needed is None.  With `order` (of
     `route`) the places that no slot takes get zeros; without it every place must be some slot's."""
-    import torch
     device = values.device
-    _on(device, dy=dy, slots=slots, weights=weights, order=order)
+    _on(device, dy, slots, weights, order)
     code = _dtype(values, "values")
-    n_values, stride = _rows(values, "values")
-    d = values.shape[1]
+    n_values, d, stride = _rows(values, "values")
     n, k = slots.shape
     _whole(slots, "slots", torch.int32, (n, k))
     if weights is not None:
@@ -277,7 +260,7 @@ def combine_gradient(dy, values, slots, weights=None, order=None, need_dvalues=T
             raise ValueError(f"order says {n * k} places, values has {n_values}")
     if dy.dtype != values.dtype or dy.shape[0] != n:
         raise ValueError(f"dy must be [{n}, {d}] of {values.dtype}")
-    _, dy_stride = _rows(dy, "dy", d)
+    _, _, dy_stride = _rows(dy, "dy", d)
     if not need_dvalues and not need_dweights:
         raise ValueError("neither gradient is asked for")
     dvalues = torch.empty(n_values, d, dtype=values.dtype, device=device) if need_dvalues else None
@@ -298,7 +281,6 @@ class State8(NamedTuple):
 
 def adamw_state(param, bits=32):
     """(first, second) averages of a tensor before its first step: float32 tensors, or State8 with bits=8."""
-    import torch
     if bits == 32:
         return torch.zeros(param.shape, dtype=torch.float32, device=param.device), torch.zeros(param.shape, dtype=torch.float32, device=param.device)
     if bits != 8:
@@ -311,7 +293,6 @@ def adamw_state(param, bits=32):
 def adamw_step(params, grads, first, second, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_scale=None, stream=None):
     """nomad_adamw_step: one step, in place, over all of the tensors at once.  first and second: the averages of `adamw_state`
     (all in 32 bits, or all in 8); step counts from 1; grad_scale: None or a float32 tensor of one element on the GPU."""
-    import torch
     params, grads, first, second = list(params), list(grads), list(first), list(second)
     if not len(params) == len(grads) == len(first) == len(second):
         raise ValueError("params, grads, first and second must be lists of the same length")
@@ -319,20 +300,20 @@ def adamw_step(params, grads, first, second, step, lr=1e-3, betas=(0.9, 0.999), 
         return
     eight = not isinstance(first[0], torch.Tensor)
     device = params[0].device
-    _on(device, grad_scale=grad_scale)
+    _on(device, grad_scale)
     if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
         raise ValueError("grad_scale must be one float32 element")
     # every check is a pass over all tensors by one C function: a step over a hundred small tensors takes the host longer than the GPU
     tensors = params + grads
     if eight:
-        if any(map(_is_tensor, first)) or any(map(_is_tensor, second)):
+        if any(isinstance(s, torch.Tensor) for s in itertools.chain(first, second)):
             raise ValueError("the states must all be in 32 bits, or all in 8")
         m, m_scale = [s[0] for s in first], [s[1] for s in first]
         v, v_scale = [s[0] for s in second], [s[1] for s in second]
         tensors += m + v + m_scale + v_scale
         wanted = ((m, {torch.int8}), (v, {torch.uint8}), (m_scale, {torch.float32}), (v_scale, {torch.float32}))
     else:
-        if not (all(map(_is_tensor, first)) and all(map(_is_tensor, second))):
+        if not (_all_tensors(first) and _all_tensors(second)):
             raise ValueError("the states must all be in 32 bits, or all in 8")
         m, v = first, second
         tensors += m + v
@@ -349,7 +330,7 @@ def adamw_step(params, grads, first, second, step, lr=1e-3, betas=(0.9, 0.999), 
         blocks = [-(-n // BLOCK) for n in sizes]
         if any(list(map(torch.Tensor.numel, which)) != blocks for which in (m_scale, v_scale)):
             raise ValueError(f"8-bit states have a scale for every {BLOCK} elements")
-    codes = _dtypes()
+    codes = _DTYPES
     kinds = list(zip(map(_get_dtype, params), map(_get_dtype, grads)))
     for p, g in set(kinds):
         if p not in codes or g not in codes or (g != p and torch.float32 not in (p, g)):
@@ -360,16 +341,14 @@ def adamw_step(params, grads, first, second, step, lr=1e-3, betas=(0.9, 0.999), 
     rows = zip(map(pointer, params), map(pointer, grads), map(pointer, m), map(pointer, v), map(pointer, m_scale) if eight else none,
                map(pointer, v_scale) if eight else none, sizes, map(words.__getitem__, kinds))
     flat = array.array("q", itertools.chain.from_iterable(rows))
-    table = (binding.AdamWTensor * count).from_buffer(flat)
     st = _stream(device, stream, tensors + [grad_scale])
-    options = binding.AdamWOptions(C.sizeof(binding.AdamWOptions), 8 if eight else 32, int(step), float(lr), float(betas[0]), float(betas[1]), float(eps),
-                                   float(weight_decay), grad_scale.data_ptr() if grad_scale is not None else None, st or None, device.index)
-    _check(load_library().nomad_adamw_step(table, count, C.byref(options)), "nomad_adamw_step")
+    options = binding.ADAMW_OPTIONS.pack(binding.ADAMW_OPTIONS.size, 8 if eight else 32, int(step), float(lr), float(betas[0]), float(betas[1]), float(eps),
+                                         float(weight_decay), grad_scale.data_ptr() if grad_scale is not None else 0, st, device.index)
+    _check(load_library().nomad_adamw_step(flat.buffer_info()[0], count, options), "nomad_adamw_step")
 
 
 def adamw_state_values(states, stream=None):
     """nomad_adamw_state_values: 8-bit averages (a list of State8, all first or all second ones) as float32 tensors."""
-    import torch
     states = [State8(*s) for s in states]
     if not states:
         return []
@@ -379,7 +358,7 @@ def adamw_state_values(states, stream=None):
         raise ValueError("codes are int8 (first averages) or uint8 (second)")
     for s in states:
         n = s.codes.numel()
-        _on(device, codes=s.codes, scales=s.scales)
+        _on(device, s.codes, s.scales)
         if s.codes.dtype != dtype or not s.codes.is_contiguous():
             raise ValueError("codes must be contiguous, and all first or all second averages")
         _whole(s.scales, "scales", torch.float32, (-(-n // BLOCK),))

@@ -57,3 +57,39 @@ def test_plans(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Wextra", "-I" + os.path.join(ROOT, "paper_2505_15511_amd", "csrc"), str(src), "-o", str(exe)], check=True)
     run = subprocess.run([str(exe)], capture_output=True, text=True)
     assert run.returncode == 0 and run.stdout == "ok\n", run.returncode
+
+
+LAYOUT = r"""
+#include <stdio.h>
+#include <stddef.h>
+#include "nomad.h"
+int main(void) {
+    printf("%zu %zu %zu %zu\n", sizeof(nomad_grouped_product_args), sizeof(nomad_grouped_gradient_args), sizeof(nomad_adamw_tensor), sizeof(nomad_adamw_options));
+    printf("%zu %zu %zu %zu\n", offsetof(nomad_grouped_product_args, rows), offsetof(nomad_grouped_product_args, w), offsetof(nomad_grouped_product_args, z_stride),
+           offsetof(nomad_grouped_product_args, device));
+    printf("%zu %zu %zu %zu\n", offsetof(nomad_grouped_gradient_args, rows), offsetof(nomad_grouped_gradient_args, dy), offsetof(nomad_grouped_gradient_args, workspace_bytes),
+           offsetof(nomad_grouped_gradient_args, device));
+    printf("%zu %zu %zu %zu\n", offsetof(nomad_adamw_tensor, n), offsetof(nomad_adamw_tensor, g_dtype), offsetof(nomad_adamw_options, lr), offsetof(nomad_adamw_options, device));
+    return 0;
+}
+"""
+
+
+def test_argument_layouts(tmp_path):
+    """What the binding packs is what the header declares."""
+    import struct
+
+    from paper_2505_15511_amd import binding as b
+    if not shutil.which("gcc"):
+        pytest.skip("no C compiler")
+    src, exe = tmp_path / "layout.c", tmp_path / "layout"
+    src.write_text(LAYOUT)
+    subprocess.run(["gcc", "-std=c99", "-I" + os.path.join(ROOT, "include"), str(src), "-o", str(exe)], check=True)
+    said = [[int(v) for v in line.split()] for line in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.splitlines()]
+    assert said[0] == [b.GROUPED_PRODUCT_ARGS.size, b.GROUPED_GRADIENT_ARGS.size, b.ADAMW_TENSOR.size, b.ADAMW_OPTIONS.size]
+
+    def at(fmt, part):                                         # offset of the field behind the first `part` of a format
+        return struct.calcsize("@" + part + "0" + fmt)
+    assert said[1] == [at("q", "I7i"), at("P", "I7i2q3Pq"), at("q", "I7i2q3PqP3qPqPqPqP"), at("i", "I7i2q3PqP3qPqPqPqPqP")]
+    assert said[2] == [at("q", "I6i4x"), at("P", "I6i4x2q2P"), at("q", "I6i4x2q2PPqPqPPP"), at("i", "I6i4x2q2PPqPqPPPqP")]
+    assert said[3] == [at("q", "6P"), at("i", "6Pqi"), at("d", "Iiq"), at("i", "Iiq5dPP")]
