@@ -93,7 +93,6 @@ __device__ __forceinline__ float activation_slope(float z) {
 struct Item {
     int64_t begin, end;   // rows of the group
     int32_t group;        // n_groups: rows of no group
-    int32_t index;        // of this item among the group's
     int32_t first;        // items before this group's
     int32_t items;        // the group has
 };
@@ -127,22 +126,18 @@ __device__ __forceinline__ int32_t group_items(int64_t begin, int64_t end, int32
 
 __device__ __forceinline__ int32_t count_items(const int32_t* offsets, int32_t n_groups, int64_t rows, int32_t step, int32_t least, bool tail, int lane) {
     const int32_t groups = n_groups + (tail ? 1 : 0);
-    int32_t total = 0;
-    for (int32_t g0 = 0; g0 < groups; g0 += 64) {
-        const int32_t e = g0 + lane;
-        int32_t items = 0;
-        if (e < groups) items = group_items(group_end(offsets, e, n_groups, rows), group_end(offsets, e + 1, n_groups, rows), step, least, e == n_groups);
-        total += of_lane(wave_inclusive(items, lane), 63);
-    }
-    return total;
+    int32_t mine = 0;
+#pragma unroll 4
+    for (int32_t e = lane; e < groups; e += 64)
+        mine += group_items(group_end(offsets, e, n_groups, rows), group_end(offsets, e + 1, n_groups, rows), step, least, e == n_groups);
+    return of_lane(wave_inclusive(mine, lane), 63);
 }
-// Item number `at` of the list (group -1 where it is beyond it)
-__device__ __forceinline__ Item find_item(const int32_t* offsets, int32_t n_groups, int64_t rows, int32_t step, int32_t least, bool tail, int32_t at, int lane) {
+// Item number `at` of the list (group -1 where it is beyond it).  `it`: an item found before, no later than this one, or one with
+// group 0 and first 0: the search goes on from its group.
+__device__ __forceinline__ void find_item(Item& it, const int32_t* offsets, int32_t n_groups, int64_t rows, int32_t step, int32_t least, bool tail, int32_t at, int lane) {
     const int32_t groups = n_groups + (tail ? 1 : 0);
-    Item it;
-    it.group = -1;
-    int32_t before = 0;
-    for (int32_t g0 = 0; g0 < groups; g0 += 64) {
+    int32_t before = it.first;
+    for (int32_t g0 = it.group; g0 < groups; g0 += 64) {
         const int32_t e = g0 + lane;
         int64_t begin = 0, end = 0;
         int32_t items = 0;
@@ -161,12 +156,11 @@ __device__ __forceinline__ Item find_item(const int32_t* offsets, int32_t n_grou
             if (it.end < it.begin) it.end = it.begin;
             it.first = of_lane(upto - items, who);
             it.items = of_lane(items, who);
-            it.index = at - it.first;
-            break;
+            return;
         }
         before = of_lane(upto, 63);
     }
-    return it;
+    it.group = -1;
 }
 
 // ---- operands: a tile of TILE rows and 128 bytes of k, in LDS, from global memory
@@ -468,14 +462,6 @@ struct ProductArgs {
     int32_t n_groups, in, out, activation;
 };
 
-// The first n of N columns to memory, one by one (results whose rows are not made of whole 16 bytes)
-template <typename O, int N>
-__device__ __forceinline__ void store_columns(O* to, const float* v, int n) {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (i < n) to[i] = (O)v[i];
-}
-
 // A wavefront's 16 rows of finished values to memory in whole rows: a matrix instruction leaves 16 consecutive lanes with 16
 // rows, and stores go out 16 lanes at a time, so rows pass through LDS first and leave 128 bytes and more side by side (pieces of 16 bytes
 // straight from the registers were written to memory 1.4 times, and a large product took 15 % longer).  They pass the caches by:
@@ -495,8 +481,21 @@ struct Rows16 {
             __builtin_memcpy(__builtin_assume_aligned(patch + row * kCols * (int)sizeof(X) + (((byte >> 4) ^ (row & kMask)) << 4) + (byte & 15), sizeof(part)), part, sizeof(part));
         }
     }
-    // rows 0 .. count - 1 of the 16, columns below `columns` from `to` on
+    // rows 0 .. count - 1 of the 16, columns below `columns` from `to` on; whole: 16 aligned bytes at a time, otherwise one by one,
+    // neighbours by neighbouring lanes
+    template <bool WHOLE>
     static __device__ __forceinline__ void send(const char* patch, X* to, int64_t stride, int count, int columns, int lane) {
+        if (!WHOLE) {
+            constexpr int rows = kCols >= 64 ? 1 : 64 / kCols, across = kCols >= 64 ? kCols / 64 : 1;   // at a time, steps a row
+#pragma unroll
+            for (int r = 0; r < 16; r += rows)
+#pragma unroll
+                for (int c = 0; c < across; ++c) {
+                    const int row = r + (kCols >= 64 ? 0 : lane / kCols), col = kCols >= 64 ? 64 * c + lane : lane % kCols, byte = col * (int)sizeof(X);
+                    if (row < count && col < columns) to[row * stride + col] = *(const X*)(patch + row * kCols * (int)sizeof(X) + (((byte >> 4) ^ (row & kMask)) << 4) + (byte & 15));
+                }
+            return;
+        }
         typedef uint32_t Word __attribute__((ext_vector_type(4)));
 #pragma unroll
         for (int t = 0; t < 16 * kChunks; t += 64) {
@@ -525,8 +524,7 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_product(ProductArgs
     Work work;
     typename Work::A a;
     typename Work::B b;
-    Item it;
-    it.group = -1;
+    Item it{0, 0, 0, 0, 0};
     // what is in the works: a tile whose first stage has been asked for
     int32_t row_tile = -1, group = 0, column = 0, count = 0;
     int64_t first = 0;
@@ -564,7 +562,7 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_product(ProductArgs
             column = (int32_t)(deal.at - (int64_t)tile * across) * TA;
             if (tile != row_tile) {
                 row_tile = tile;
-                if (it.group < 0 || tile >= it.first + it.items) it = find_item(p.offsets, p.n_groups, p.rows, TB, 0, true, tile, lane);
+                if (tile >= it.first + it.items) find_item(it, p.offsets, p.n_groups, p.rows, TB, 0, true, tile, lane);
                 group = it.group;
                 first = it.begin + (int64_t)(tile - it.first) * TB;
                 count = (int32_t)(it.end - first < TB ? it.end - first : TB);
@@ -606,25 +604,19 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_product(ProductArgs
 #pragma unroll
                             for (int j = 0; j < N; ++j) v[set][j] *= activation_slope<ACT>((float)z[j]);
                         } else if (p.z_out) {
-                            if (STORES) Rows16<Work, T>::put(patch, set, v[set], lane);
-                            else store_columns<T, N>((T*)p.z_out + (done_first + r) * p.z_stride + col, v[set], n);
+                            Rows16<Work, T>::put(patch, set, v[set], lane);
                         }
                     }
-                    if (STORES && !SLOPE && p.z_out)
-                        Rows16<Work, T>::send(patch, (T*)p.z_out + (done_first + r0) * p.z_stride + wave_column, p.z_stride, done_count - r0, p.out - wave_column, lane);
+                    if (!SLOPE && p.z_out)
+                        Rows16<Work, T>::template send<STORES>(patch, (T*)p.z_out + (done_first + r0) * p.z_stride + wave_column, p.z_stride, done_count - r0, p.out - wave_column, lane);
 #pragma unroll
                     for (int set = 0; set < Work::kSets; ++set) {
                         if (!SLOPE && inside)
 #pragma unroll
                             for (int j = 0; j < N; ++j) v[set][j] = activate<ACT>(v[set][j]);
-                        if (STORES) {
-                            Rows16<Work, O>::put(patch, set, v[set], lane);
-                        } else {
-                            const int32_t col = done_column + Work::column(set, tid);
-                            store_columns<O, N>((O*)p.y + (done_first + r) * p.y_stride + col, v[set], r < done_count ? p.out - col : 0);
-                        }
+                        Rows16<Work, O>::put(patch, set, v[set], lane);
                     }
-                    if (STORES) Rows16<Work, O>::send(patch, (O*)p.y + (done_first + r0) * p.y_stride + wave_column, p.y_stride, done_count - r0, p.out - wave_column, lane);
+                    Rows16<Work, O>::template send<STORES>(patch, (O*)p.y + (done_first + r0) * p.y_stride + wave_column, p.y_stride, done_count - r0, p.out - wave_column, lane);
                 }
             };
             const int act = inside ? p.activation : (int)kNone;   // (one copy of the code for each, outside the loops over rows)
@@ -653,9 +645,10 @@ __global__ void __launch_bounds__(64 * kFewWaves) k_grouped_few(ProductArgs p) {
     const int32_t across = (p.out + 15) / 16;
     const int64_t block = block_number();
     const int32_t tile = (int32_t)(block / across), column = (int32_t)(block - (int64_t)tile * across) * 16;
-    const Item it = find_item(p.offsets, p.n_groups, p.rows, 16, 0, true, tile, lane);
+    Item it{0, 0, 0, 0, 0};
+    find_item(it, p.offsets, p.n_groups, p.rows, 16, 0, true, tile, lane);
     if (it.group < 0) return;
-    const int64_t first = it.begin + (int64_t)it.index * 16;
+    const int64_t first = it.begin + (int64_t)(tile - it.first) * 16;
     const int32_t count = (int32_t)(it.end - first < 16 ? it.end - first : 16);
     const bool inside = it.group < p.n_groups;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -738,24 +731,38 @@ __device__ __forceinline__ int64_t slot_of(int64_t part_begin, int32_t slot_bits
 struct Unit {
     int64_t begin;
     int32_t group, count, parts;
+    int32_t length, from, before;   // where the search for the next one begins: class of lengths, group, parts before it
 };
 // Parts in the order in which they are taken: long ones first (four classes by length), so that what is left at the end is short.
-// Number `at` of them, or, with group -1 beyond the last, their number in `parts`.
-__device__ __forceinline__ Unit find_unit(const GradientArgs& p, int32_t at, int lane) {
-    int32_t before = 0;
-    for (int32_t length = 0; length < 4; ++length)
-        for (int32_t g0 = 0; g0 < p.n_groups; g0 += 64) {
+__device__ __forceinline__ int32_t length_class(int32_t parts, int32_t count, int32_t most) {   // (a part of a long group has more than half of `most` rows)
+    return parts > 1 || count > most / 2 ? 0 : count > most / 4 ? 1 : count > most / 8 ? 2 : 3;
+}
+__device__ __forceinline__ int32_t rows_of_group(const GradientArgs& p, int32_t e, int64_t& begin) {
+    begin = group_end(p.offsets, e, p.n_groups, p.rows);
+    const int64_t rows = group_end(p.offsets, e + 1, p.n_groups, p.rows) - begin;
+    return rows < 0 ? 0 : (int32_t)rows;
+}
+__device__ __forceinline__ int32_t count_units(const GradientArgs& p, int lane) {
+    int32_t mine = 0;
+#pragma unroll 4
+    for (int32_t e = lane; e < p.n_groups; e += 64) {
+        int64_t begin;
+        mine += parts_of(rows_of_group(p, e, begin), p.most);
+    }
+    return of_lane(wave_inclusive(mine, lane), 63);
+}
+// Part number `at` of that order, which there is, and which is no earlier than the one in `u`
+__device__ __forceinline__ void find_unit(const GradientArgs& p, Unit& u, int32_t at, int lane) {
+    int32_t before = u.before, g0 = u.from;
+    for (int32_t length = u.length; length < 4; ++length, g0 = 0)
+        for (; g0 < p.n_groups; g0 += 64) {
             const int32_t e = g0 + lane;
             int64_t begin = 0;
             int32_t count = 0, parts = 0, mine = 0;
             if (e < p.n_groups) {
-                begin = group_end(p.offsets, e, p.n_groups, p.rows);
-                const int64_t rows = group_end(p.offsets, e + 1, p.n_groups, p.rows) - begin;
-                count = rows < 0 ? 0 : (int32_t)rows;
+                count = rows_of_group(p, e, begin);
                 parts = parts_of(count, p.most);
-                // (a part of a long group has more than half of `most` rows)
-                const int32_t is = parts > 1 || count > p.most / 2 ? 0 : count > p.most / 4 ? 1 : count > p.most / 8 ? 2 : 3;
-                if (is == length) mine = parts;
+                if (length_class(parts, count, p.most) == length) mine = parts;
             }
             const int32_t upto = before + wave_inclusive(mine, lane);
             const uint64_t mask = __ballot(upto > at);
@@ -763,17 +770,18 @@ __device__ __forceinline__ Unit find_unit(const GradientArgs& p, int32_t at, int
                 const int who = __builtin_ctzll(mask);
                 const int64_t b = of_lane(begin, who);
                 const int32_t c = of_lane(count, who);
-                Unit u;
                 u.parts = of_lane(parts, who);
                 const int32_t part = at - of_lane(upto - mine, who);
                 u.group = g0 + who;
                 u.begin = part_begin(b, c, part, u.parts);
                 u.count = (int32_t)(part_begin(b, c, part + 1, u.parts) - u.begin);
-                return u;
+                u.length = length;
+                u.from = g0;
+                u.before = before;
+                return;
             }
             before = of_lane(upto, 63);
         }
-    return Unit{0, -1, 0, before};
 }
 
 // dW = sum over the group's rows of dy^T x: tiles of TA columns of x and TB of dy.  The tiles of a part go to one XCD, side by side: they read
@@ -785,12 +793,12 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_gradient(GradientAr
     __shared__ uint4 a0[TA * kTileChunks], a1[TA * kTileChunks], b0[TB * kTileChunks], b1[TB * kTileChunks];
     const int lane = threadIdx.x & 63, tid = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 64 + lane;   // (the wavefront's number in a scalar register)
     const int32_t across = (p.in + TA - 1) / TA, tiles = across * ((p.out + TB - 1) / TB);
-    const int32_t units = find_unit(p, 0x7fffffff, lane).parts;
+    const int32_t units = count_units(p, lane);
     const int32_t xcds = gridDim.x % 8 == 0 ? 8 : 1, xcd = (int32_t)blockIdx.x % xcds, local = (int32_t)blockIdx.x / xcds, locals = (int32_t)gridDim.x / xcds;
     Work work;
     typename Work::A a;
     typename Work::B b;
-    Unit unit{0, -1, 0, 0};
+    Unit unit{0, -1, 0, 0, 0, 0, 0};
     int32_t unit_at = -1, a_first = 0, b_first = 0;
     int32_t turn = 0;
     for (bool have = false;; have = true) {
@@ -812,7 +820,7 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_gradient(GradientAr
         const bool more = next < units;
         if (more) {
             const int32_t tile = (int32_t)(t - band * tiles);
-            if (next != unit_at) unit = find_unit(p, (int32_t)next, lane);
+            if (next != unit_at) find_unit(p, unit, (int32_t)next, lane);
             unit_at = (int32_t)next;
             a_first = tile % across * TA;
             b_first = tile / across * TB;
@@ -839,18 +847,16 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_gradient(GradientAr
                 typedef typename std::remove_pointer<decltype(to)>::type X;
 #pragma unroll
                 for (int y = 0; y < Work::kFb; ++y) {
-                    const int32_t r0 = done_b + Work::row(y, tid & ~63), r = done_b + Work::row(y, tid);
+                    const int32_t r0 = done_b + Work::row(y, tid & ~63);
                     if (r0 >= p.out) continue;
 #pragma unroll
                     for (int set = 0; set < Work::kSets; ++set) {
-                        const int32_t col = done_a + Work::column(set, tid);
                         float v[N];
 #pragma unroll
                         for (int j = 0; j < N; ++j) v[j] = work.at(set, y, j);
-                        if (STORES) Rows16<Work, X>::put(patch, set, v, lane);
-                        else store_columns<X, N>(to + (int64_t)r * p.in + col, v, r < p.out ? p.in - col : 0);
+                        Rows16<Work, X>::put(patch, set, v, lane);
                     }
-                    if (STORES) Rows16<Work, X>::send(patch, to + (int64_t)r0 * p.in + wave_column, p.in, p.out - r0, p.in - wave_column, lane);
+                    Rows16<Work, X>::template send<STORES>(patch, to + (int64_t)r0 * p.in + wave_column, p.in, p.out - r0, p.in - wave_column, lane);
                 }
             };
             if (done.parts == 1) out((O*)p.dw + (int64_t)done.group * p.out * p.in);
