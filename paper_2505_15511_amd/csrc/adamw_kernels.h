@@ -19,7 +19,9 @@ namespace nomad_adamw {
 
 constexpr int kTensors = 64;              // a launch: their addresses are its arguments (under 4 KB)
 constexpr int kThreads = 256, kPer = 8;   // lanes a workgroup, elements a lane
-constexpr int kChunk = kThreads * kPer;   // elements a workgroup
+constexpr int kChunk = kThreads * kPer;   // elements a workgroup takes at a time
+constexpr int kTurns = 4;                 // and how often, where there are enough for every compute unit: 2,048 elements are
+                                          // little beside the search for their tensor and the first load's way
 constexpr int kBlock = 256;               // elements a scale
 constexpr int kLanes = kBlock / kPer;
 
@@ -39,7 +41,7 @@ struct Scalars {
 struct Batch {
     Tensor t[kTensors];
     uint32_t first[kTensors + 1];   // workgroup of each tensor
-    int32_t count;
+    int32_t count, turns;
     Scalars s;
 };
 
@@ -89,25 +91,29 @@ __device__ __forceinline__ uint32_t block_most(uint32_t bits) {
 __device__ __forceinline__ float scale_of(uint32_t bits) {
     return bits < 0x00800000u ? 0.f : __uint_as_float(bits);
 }
+// The root is a unit off at most, its whole number by one at a border: that is put right.  (No branches; c = 0 has no lower border;
+// fmaxf makes a NaN, whose scale is one already, 0.)
 __device__ __forceinline__ int encode_first(float m, float factor) {
 #pragma clang fp contract(off)
-    const float t = fabsf(m) * factor;
-    float c = rintf(__builtin_amdgcn_sqrtf(t));
-    const float up = c + 0.5f, down = c - 0.5f;
-    c += (t >= up * up ? 1.f : 0.f) - (t < down * down && c > 0.f ? 1.f : 0.f);
-    const int code = c == c ? (int)c : 0;
+    const float t = fabsf(m) * factor, c = fmaxf(rintf(__builtin_amdgcn_sqrtf(t)), 0.f);
+    const float up = c + 0.5f, down = fmaxf(c - 0.5f, 0.f);
+    int code = (int)c;
+    code += t >= up * up;
+    code -= t < down * down;
     return m < 0.f ? -code : code;
 }
-__device__ __forceinline__ uint32_t encode_second(float v, float factor) {
+// least: what v is above where its code is at least 1
+__device__ __forceinline__ uint32_t encode_second(float v, float factor, float least) {
 #pragma clang fp contract(off)
-    const float t = v * factor;
-    float c = rintf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(t)));
-    float up = c + 0.5f, down = c - 0.5f;
+    const float t = v * factor, c = fmaxf(rintf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(t))), 0.f);
+    float up = c + 0.5f, down = fmaxf(c - 0.5f, 0.f);
     up = up * up;
     down = down * down;
-    c += (t >= up * up ? 1.f : 0.f) - (t < down * down && c > 0.f ? 1.f : 0.f);
-    const uint32_t code = c == c ? (uint32_t)c : 0u;
-    return v > 0.f && factor > 0.f && code == 0 ? 1u : code;
+    int code = (int)c;
+    code += t >= up * up;
+    code -= t < down * down;
+    const int one = v > least;
+    return (uint32_t)(code > one ? code : one);
 }
 
 template <typename P, typename G, bool EIGHT, bool WHOLE>
@@ -151,10 +157,11 @@ __device__ __forceinline__ void step8(const Tensor& t, const Scalars& s, int64_t
         }
         const float ms = scale_of(block_most(m_most)), vs = scale_of(block_most(v_most));
         const float mf = ms == 0.f ? 0.f : 16129.f / ms, vf = vs == 0.f ? 0.f : 4228250625.f / vs;
+        const float least = vs > 0.f ? 0.f : __builtin_inff();
         int8_t mc[kPer];
         uint8_t vc[kPer];
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) { mc[i] = (int8_t)encode_first(m[i], mf); vc[i] = (uint8_t)encode_second(v[i], vf); }
+        for (int i = 0; i < kPer; ++i) { mc[i] = (int8_t)encode_first(m[i], mf); vc[i] = (uint8_t)encode_second(v[i], vf, least); }
         store8<int8_t, WHOLE>((int8_t*)t.m + at, n, mc);
         store8<uint8_t, WHOLE>((uint8_t*)t.v + at, n, vc);
         if (n > 0 && at % kBlock == 0) { t.m_scale[at / kBlock] = ms; t.v_scale[at / kBlock] = vs; }
@@ -175,11 +182,14 @@ __global__ void __launch_bounds__(kThreads) k_adamw(Batch b) {
         else hi = mid;
     }
     const Tensor t = b.t[lo];
-    const int64_t first = (int64_t)(blockIdx.x - b.first[lo]) * kChunk, at = first + (int64_t)threadIdx.x * kPer;
-    const bool whole = first + kChunk <= t.n && aligned(t.p, sizeof(P) * 4 < 16 ? sizeof(P) * kPer : 16) && aligned(t.g, sizeof(G) * 4 < 16 ? sizeof(G) * kPer : 16) &&
-                       aligned(t.m, EIGHT ? 8 : 16) && aligned(t.v, EIGHT ? 8 : 16);
-    if (whole) step8<P, G, EIGHT, true>(t, b.s, at, kPer);
-    else step8<P, G, EIGHT, false>(t, b.s, at, (int)(t.n - at > kPer ? kPer : t.n - at));   // (every lane stays: the block's largest is found by all)
+    const bool borders = aligned(t.p, sizeof(P) * 4 < 16 ? sizeof(P) * kPer : 16) && aligned(t.g, sizeof(G) * 4 < 16 ? sizeof(G) * kPer : 16) &&
+                         aligned(t.m, EIGHT ? 8 : 16) && aligned(t.v, EIGHT ? 8 : 16);
+    int64_t first = (int64_t)(blockIdx.x - b.first[lo]) * b.turns * kChunk;
+    for (int turn = 0; turn < b.turns && first < t.n; ++turn, first += kChunk) {
+        const int64_t at = first + (int64_t)threadIdx.x * kPer;
+        if (borders && first + kChunk <= t.n) step8<P, G, EIGHT, true>(t, b.s, at, kPer);
+        else step8<P, G, EIGHT, false>(t, b.s, at, (int)(t.n - at > kPer ? kPer : t.n - at));   // (every lane stays: the block's largest is found by all)
+    }
 }
 
 // 8-bit states as the values they stand for
