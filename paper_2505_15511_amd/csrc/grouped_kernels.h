@@ -27,7 +27,7 @@ enum Activation { kNone = 0, kRelu = 1, kSilu = 2, kGelu = 3 };
 // Workgroup number of a launch with more of them than one dimension takes (grid_of)
 __device__ __forceinline__ int64_t block_number() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
 
-// ---- element types: 16 bytes are one fragment of a matrix step (two or four instructions' worth for float32)
+// ---- element types: 16 bytes are one fragment of a matrix step (one instruction, four for float32)
 
 template <typename T> struct Elem;
 template <> struct Elem<__bf16> {
@@ -53,9 +53,6 @@ template <> struct Elem<float> {
     }
     static __device__ __forceinline__ uint4 ones() { return make_uint4(0x3f800000u, 0x3f800000u, 0x3f800000u, 0x3f800000u); }
 };
-
-template <typename T>
-__device__ __forceinline__ float to_f32(T v) { return (float)v; }
 
 template <int V> struct Constant { static constexpr int value = V; };
 
@@ -88,8 +85,8 @@ __device__ __forceinline__ float activation_slope(float z) {
 
 // ---- the groups' work items
 
-// Items of a launch: group e has ceil(its rows / step) of them (at least `least`), and one group behind the last stands for the
-// rows that belong to no group.  Every wavefront finds the item of its workgroup by itself, 64 groups at a time.
+// Items of a product: group e has ceil(its rows / step) of them, and one group behind the last stands for the rows that belong to
+// no group.  Every wavefront finds the item of its workgroup by itself, 64 groups at a time.
 struct Item {
     int64_t begin, end;   // rows of the group
     int32_t group;        // n_groups: rows of no group
@@ -118,33 +115,26 @@ __device__ __forceinline__ int32_t wave_inclusive(int32_t v, int lane) {
     return v;
 }
 
-__device__ __forceinline__ int32_t group_items(int64_t begin, int64_t end, int32_t step, int32_t least, bool tail) {
-    const int64_t count = end > begin ? end - begin : 0;
-    const int32_t items = (int32_t)((count + step - 1) / step);
-    return tail ? items : items < least ? least : items;
-}
+__device__ __forceinline__ int32_t items_of(int64_t begin, int64_t end, int32_t step) { return end > begin ? (int32_t)((end - begin + step - 1) / step) : 0; }
 
-__device__ __forceinline__ int32_t count_items(const int32_t* offsets, int32_t n_groups, int64_t rows, int32_t step, int32_t least, bool tail, int lane) {
-    const int32_t groups = n_groups + (tail ? 1 : 0);
+__device__ __forceinline__ int32_t count_items(const int32_t* offsets, int32_t n_groups, int64_t rows, int32_t step, int lane) {
     int32_t mine = 0;
 #pragma unroll 4
-    for (int32_t e = lane; e < groups; e += 64)
-        mine += group_items(group_end(offsets, e, n_groups, rows), group_end(offsets, e + 1, n_groups, rows), step, least, e == n_groups);
+    for (int32_t e = lane; e <= n_groups; e += 64) mine += items_of(group_end(offsets, e, n_groups, rows), group_end(offsets, e + 1, n_groups, rows), step);
     return of_lane(wave_inclusive(mine, lane), 63);
 }
 // Item number `at` of the list (group -1 where it is beyond it).  `it`: an item found before, no later than this one, or one with
 // group 0 and first 0: the search goes on from its group.
-__device__ __forceinline__ void find_item(Item& it, const int32_t* offsets, int32_t n_groups, int64_t rows, int32_t step, int32_t least, bool tail, int32_t at, int lane) {
-    const int32_t groups = n_groups + (tail ? 1 : 0);
+__device__ __forceinline__ void find_item(Item& it, const int32_t* offsets, int32_t n_groups, int64_t rows, int32_t step, int32_t at, int lane) {
     int32_t before = it.first;
-    for (int32_t g0 = it.group; g0 < groups; g0 += 64) {
+    for (int32_t g0 = it.group; g0 <= n_groups; g0 += 64) {
         const int32_t e = g0 + lane;
         int64_t begin = 0, end = 0;
         int32_t items = 0;
-        if (e < groups) {
+        if (e <= n_groups) {
             begin = group_end(offsets, e, n_groups, rows);
             end = group_end(offsets, e + 1, n_groups, rows);
-            items = group_items(begin, end, step, least, e == n_groups);
+            items = items_of(begin, end, step);
         }
         const int32_t upto = before + wave_inclusive(items, lane);
         const uint64_t mask = __ballot(upto > at);
@@ -153,7 +143,6 @@ __device__ __forceinline__ void find_item(Item& it, const int32_t* offsets, int3
             it.group = g0 + who;
             it.begin = of_lane(begin, who);
             it.end = of_lane(end, who);
-            if (it.end < it.begin) it.end = it.begin;
             it.first = of_lane(upto - items, who);
             it.items = of_lane(items, who);
             return;
@@ -206,7 +195,8 @@ struct Source {
 };
 
 // TILE rows (KC) or columns (not KC) by one stage of k, for NT threads.  PICKED: source rows anywhere (KC: a pointer each; otherwise
-// the numbers of 64 rows at a time in a register of the wavefront, the next 64 on their way).  ASYNC: loads go to LDS directly, whole 16-byte chunks; otherwise through registers, element by element where a chunk is cut off.
+// the numbers of 64 rows at a time in a register of the wavefront, the next 64 on their way).  ASYNC: loads go to LDS directly, whole
+// 16-byte chunks; otherwise through registers, element by element where a chunk is cut off.
 template <typename T, int TILE, bool KC, bool PICKED, int Q, bool ASYNC, int NT>
 struct Operand {
     static constexpr int kEpc = 16 / (int)sizeof(T);             // elements a chunk
@@ -511,6 +501,10 @@ struct Rows16 {
 // y = act(x W^T + b), or (x W^T) act'(z).  Workgroups stay and take tiles in turn, the column tiles of a row tile next to each
 // other: x comes from memory once, a group's weights stay in the XCD's L2.  The next tile's first stage is asked for before the results
 // of this one are finished and stored.
+//
+// What bounds it: the matrix cores, and what does not go on under them, a tile's activation and stores.  524,288 rows of 768 -> 2,048 in
+// bfloat16, gathered, with bias and SiLU: 2.0 ms, 830 TFLOP/s (a plain library product of that size 1.57 ms); without the SiLU 1.88;
+// 48 rows through 64 experts of that size 32 us, 6.3 TB/s of weights.
 // LOADS, STORES: rows are made of whole aligned 16-byte chunks where they are read (straight to LDS), where they are written; otherwise
 // element by element at the ends.
 template <typename T, typename O, int TA, int TB, int WA, int WB, bool W_KC, bool LOADS, bool STORES>
@@ -520,7 +514,7 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_product(ProductArgs
     __shared__ uint4 a0[TA * kTileChunks], a1[TA * kTileChunks], b0[TB * kTileChunks], b1[TB * kTileChunks];
     const int lane = threadIdx.x & 63, tid = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 64 + lane;   // (the wavefront's number in a scalar register)
     const int32_t across = (p.out + TA - 1) / TA;
-    Deal deal = my_items((int64_t)count_items(p.offsets, p.n_groups, p.rows, TB, 0, true, lane) * across);
+    Deal deal = my_items((int64_t)count_items(p.offsets, p.n_groups, p.rows, TB, lane) * across);
     Work work;
     typename Work::A a;
     typename Work::B b;
@@ -562,7 +556,7 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_product(ProductArgs
             column = (int32_t)(deal.at - (int64_t)tile * across) * TA;
             if (tile != row_tile) {
                 row_tile = tile;
-                if (tile >= it.first + it.items) find_item(it, p.offsets, p.n_groups, p.rows, TB, 0, true, tile, lane);
+                if (tile >= it.first + it.items) find_item(it, p.offsets, p.n_groups, p.rows, TB, tile, lane);
                 group = it.group;
                 first = it.begin + (int64_t)(tile - it.first) * TB;
                 count = (int32_t)(it.end - first < TB ? it.end - first : TB);
@@ -634,8 +628,8 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_product(ProductArgs
 
 // The same for few rows, where the groups' weights are read once and there are too few tiles for all compute units: a workgroup takes 16
 // rows and 16 columns, its wavefronts share k, two steps (128 bytes of every row) at a time, straight from memory to
-// registers, and add up in LDS.  Latency is all it costs: one row of bfloat16 through two experts of 768 x 2,048 takes 7 us, 15 in
-// tiles of 128.
+// registers, and add up in LDS.  Latency is all it costs: one row of bfloat16 through two experts of 768 x 2,048 takes 5.6 us (6.3 MB of
+// weights, 1.2 us at the rate of a large copy), 15.4 in tiles of 128.
 constexpr int kFewWaves = 8;
 template <typename T, typename O>
 __global__ void __launch_bounds__(64 * kFewWaves) k_grouped_few(ProductArgs p) {
@@ -646,7 +640,7 @@ __global__ void __launch_bounds__(64 * kFewWaves) k_grouped_few(ProductArgs p) {
     const int64_t block = block_number();
     const int32_t tile = (int32_t)(block / across), column = (int32_t)(block - (int64_t)tile * across) * 16;
     Item it{0, 0, 0, 0, 0};
-    find_item(it, p.offsets, p.n_groups, p.rows, 16, 0, true, tile, lane);
+    find_item(it, p.offsets, p.n_groups, p.rows, 16, tile, lane);
     if (it.group < 0) return;
     const int64_t first = it.begin + (int64_t)(tile - it.first) * 16;
     const int32_t count = (int32_t)(it.end - first < 16 ? it.end - first : 16);
@@ -786,6 +780,8 @@ __device__ __forceinline__ void find_unit(const GradientArgs& p, Unit& u, int32_
 
 // dW = sum over the group's rows of dy^T x: tiles of TA columns of x and TB of dy.  The tiles of a part go to one XCD, side by side: they read
 // the same rows.  Workgroups stay and take every so many-th tile of their XCD, in turn from either end, as the parts get shorter.
+// Both operands are turned on their way out of LDS.  524,288 rows, 2,048 x 768 in bfloat16: 2.0 ms, 810 TFLOP/s; 200,006 rows in 256 groups,
+// 512 x 768: 0.29 ms, where rows and results alone are 0.15 at the rate of a large copy.
 template <typename T, typename O, int TA, int TB, int WA, int WB, bool LOADS, bool STORES>
 __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_gradient(GradientArgs p) {
     typedef Tile<T, O, TA, TB, WA, WB, false, true, false, false, LOADS> Work;

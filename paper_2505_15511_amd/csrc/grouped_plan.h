@@ -6,9 +6,9 @@
 
 namespace nomad_grouped {
 
-// Tiles of the result, columns x rows (gradients: columns of x x columns of dy).  256 x 256 needs the fewest bytes from L2 an operation (31 a clock and
-// compute unit at the matrix cores' peak, of 64; 128 x 128 needs 62, and reaches 890 TFLOP/s where the large one reaches
-// 990 in bfloat16), but a unit holds only one, and it wastes more on ragged ends.
+// Tiles of the result, columns x rows (gradients: columns of x x columns of dy).  256 x 256 asks L2 for the fewest bytes an operation (31 a clock
+// and compute unit at the matrix cores' peak in bfloat16, of 64; 128 x 128 asks for 62: the gradient of 524,288 rows of 2,048 -> 768
+// runs at 1,035 against 890 TFLOP/s), but a unit holds only one, and it wastes more on ragged ends.
 enum ProductTile { kProduct256 = 0, kProduct128, kProduct64, kProduct16, kProductFew };   // 256x256, 128x128, 64x128, 16x256, few rows
 enum GradientTile { kGradient256 = 0, kGradient128, kGradient64, kGradient16 };           // 256x256, 128x128, 64x64, 128x16
 
@@ -19,9 +19,11 @@ inline int64_t tiles_of(int64_t size, int64_t tile) { return (size + tile - 1) /
 inline ProductTile plan_product(int64_t rows, int64_t groups, int64_t out, bool small, bool w_kc, int64_t units) {
     // tiles of rows there can be: no more than one a row, one a group beyond the whole ones
     const auto row_tiles = [&](int64_t tile) { return std::min(rows, rows / tile + groups); };
+    // so few that most units would have none: k is shared instead (2 rows, 768 -> 2,048 in bfloat16: 5.6 us, 15.4 in tiles of 128)
     if (w_kc && rows <= 16 * groups && row_tiles(128) * tiles_of(out, 128) < units) return kProductFew;
-    if (out <= 16) return kProduct16;
+    if (out <= 16) return kProduct16;   // (131,072 rows of 256 -> 2 in float32: 43 us, 68 in tiles of 64 columns)
     // narrow tiles read x more often, and are right where wide ones would be empty: 129 columns are three of 64, not two of 128
+    // (200,006 rows of 50 -> 129 in float32: 126 us, 150 in tiles of 128)
     if (out <= 64 || tiles_of(out, 64) * 64 * 9 < tiles_of(out, 128) * 128 * 8) return kProduct64;
     if (!small || out <= 128) return kProduct128;
     // large tiles where they are at least half full and there is one for every compute unit
@@ -40,9 +42,10 @@ struct GradientPlan {
 inline GradientPlan plan_gradient(int64_t rows, int64_t groups, int64_t in, int64_t out, bool small, int64_t units) {
     GradientPlan plan;
     const int64_t large = tiles_of(in, 256) * tiles_of(out, 256), middle = tiles_of(in, 128) * tiles_of(out, 128), little = tiles_of(in, 64) * tiles_of(out, 64);
+    // (131,072 rows, 2 x 256 in float32: 60 us, 143 in tiles of 64 x 64)
     if (out <= 16 && in > 64) { plan.tile = kGradient16; plan.tiles = tiles_of(in, 128) * tiles_of(out, 16); }
     else if (small && in > 128 && out > 128 && large * groups >= units / 2) { plan.tile = kGradient256; plan.tiles = large; }
-    else if (little * 16 < middle * 48) { plan.tile = kGradient64; plan.tiles = little; }   // a quarter less to compute, or more
+    else if (little * 16 < middle * 48) { plan.tile = kGradient64; plan.tiles = little; }   // a quarter less to compute, or more (40,022 rows, 50 x 129 in float32: 49 us, 78 in tiles of 128)
     else { plan.tile = kGradient128; plan.tiles = middle; }
     // A quarter of a compute unit's share of the whole, so that the units end together (a group of 48,000 rows, 2,048 x 768: 2.1 ms,
     // 2.5 with whole shares); but writing and reading a part's sums costs as much as about a thousand of its rows, so no

@@ -4,7 +4,8 @@
 // k_route_scan   counts of all chunks -> where every chunk's slots of every expert begin, and every expert's total
 // k_route_place  slots (row times k plus rank) into the order of their experts, stable
 // k_route_small  all of it in one workgroup
-// All are passes over the logits or over n k words: what they cost is the logits' bytes.
+// All are passes over the logits or over n k words: what they cost is the logits' bytes.  A million rows of 256 float32 logits, k = 2: 224 us for
+// the pick (4.6 TB/s), 6 + 28 for scan and places, 226 for the gradient (4.5 TB/s written).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -314,7 +315,7 @@ struct RouteGradientArgs {
     void* dlogits;             // [n, n_experts]
 };
 
-// 16 bytes, or one element, past the caches: a later kernel reads them (measured: a million rows of 256 in 4.9 TB/s against 3.8)
+// 16 bytes, or one element, past the caches: a later kernel reads them (a million rows of 256: 226 us, 273 through them)
 template <typename T, bool VEC>
 __device__ __forceinline__ void store_chunk(T* to, const T* part) {
     typedef uint32_t Word __attribute__((ext_vector_type(4)));
