@@ -91,29 +91,36 @@ __device__ __forceinline__ uint32_t block_most(uint32_t bits) {
 __device__ __forceinline__ float scale_of(uint32_t bits) {
     return bits < 0x00800000u ? 0.f : __uint_as_float(bits);
 }
-// The root is a unit off at most, its whole number by one at a border: that is put right.  (No branches; c = 0 has no lower border;
-// fmaxf makes a NaN, whose scale is one already, 0.)
-__device__ __forceinline__ int encode_first(float m, float factor) {
+// Roots by the hardware, whose last place may be off by one: `off` collects how far they lie from their whole numbers, and where none
+// is nearer to a border than that error reaches (kSure: 128 2^-23, and one and a half times that of 255 for the fourth root
+// and 2^-26 for its border), the whole numbers are the codes.  Otherwise, for one wavefront in nine, borders are compared.
+// (fmaxf makes a NaN, whose scale is one already, 0.)
+constexpr float kSureFirst = 0.49997f, kSureSecond = 0.49992f;
+__device__ __forceinline__ float root_first(float m, float factor, float& off) {
 #pragma clang fp contract(off)
-    const float t = fabsf(m) * factor, c = fmaxf(rintf(__builtin_amdgcn_sqrtf(t)), 0.f);
-    const float up = c + 0.5f, down = fmaxf(c - 0.5f, 0.f);
-    int code = (int)c;
-    code += t >= up * up;
-    code -= t < down * down;
-    return m < 0.f ? -code : code;
+    const float r = __builtin_amdgcn_sqrtf(fabsf(m) * factor), c = rintf(r);
+    off = fmaxf(off, fabsf(r - c));
+    return fmaxf(c, 0.f);
 }
-// least: what v is above where its code is at least 1
-__device__ __forceinline__ uint32_t encode_second(float v, float factor, float least) {
+__device__ __forceinline__ float root_second(float v, float factor, float& off) {
 #pragma clang fp contract(off)
-    const float t = v * factor, c = fmaxf(rintf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(t))), 0.f);
+    const float r = __builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(v * factor)), c = rintf(r);
+    off = fmaxf(off, fabsf(r - c));
+    return fmaxf(c, 0.f);
+}
+// the code of |m| factor = t from a whole number that is one off at most (c = 0 has no lower border)
+__device__ __forceinline__ float border_first(float c, float m, float factor) {
+#pragma clang fp contract(off)
+    const float t = fabsf(m) * factor, up = c + 0.5f, down = fmaxf(c - 0.5f, 0.f);
+    return c + (t >= up * up ? 1.f : 0.f) - (t < down * down ? 1.f : 0.f);
+}
+__device__ __forceinline__ float border_second(float c, float v, float factor) {
+#pragma clang fp contract(off)
+    const float t = v * factor;
     float up = c + 0.5f, down = fmaxf(c - 0.5f, 0.f);
     up = up * up;
     down = down * down;
-    int code = (int)c;
-    code += t >= up * up;
-    code -= t < down * down;
-    const int one = v > least;
-    return (uint32_t)(code > one ? code : one);
+    return c + (t >= up * up ? 1.f : 0.f) - (t < down * down ? 1.f : 0.f);
 }
 
 template <typename P, typename G, bool EIGHT, bool WHOLE>
@@ -157,11 +164,20 @@ __device__ __forceinline__ void step8(const Tensor& t, const Scalars& s, int64_t
         }
         const float ms = scale_of(block_most(m_most)), vs = scale_of(block_most(v_most));
         const float mf = ms == 0.f ? 0.f : 16129.f / ms, vf = vs == 0.f ? 0.f : 4228250625.f / vs;
-        const float least = vs > 0.f ? 0.f : __builtin_inff();
+        float off_first = 0.f, off_second = 0.f, mr[kPer], vr[kPer];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) { mr[i] = root_first(m[i], mf, off_first); vr[i] = root_second(v[i], vf, off_second); }
+        if (__any(off_first > kSureFirst || off_second > kSureSecond))
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) { mr[i] = border_first(mr[i], m[i], mf); vr[i] = border_second(vr[i], v[i], vf); }
+        const float least = vs > 0.f ? 0.f : __builtin_inff();   // what v is above where its code is at least 1
         int8_t mc[kPer];
         uint8_t vc[kPer];
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) { mc[i] = (int8_t)encode_first(m[i], mf); vc[i] = (uint8_t)encode_second(v[i], vf, least); }
+        for (int i = 0; i < kPer; ++i) {
+            mc[i] = (int8_t)(int)copysignf(mr[i], m[i]);
+            vc[i] = (uint8_t)(uint32_t)fmaxf(vr[i], v[i] > least ? 1.f : 0.f);
+        }
         store8<int8_t, WHOLE>((int8_t*)t.m + at, n, mc);
         store8<uint8_t, WHOLE>((uint8_t*)t.v + at, n, vc);
         if (n > 0 && at % kBlock == 0) { t.m_scale[at / kBlock] = ms; t.v_scale[at / kBlock] = vs; }
