@@ -5,7 +5,7 @@
 // k_route_place  slots (row times k plus rank) into the order of their experts, stable
 // k_route_small  all of it in one workgroup
 // All are passes over the logits or over n k words: what they cost is the logits' bytes.  A million rows of 256 float32 logits, k = 2: 224 us for
-// the pick (4.6 TB/s), 6 + 28 for scan and places, 226 for the gradient (4.5 TB/s written).
+// the pick (4.6 TB/s), 6 + 28 for scan and places, 187 for the gradient (5.5 TB/s written).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -315,7 +315,7 @@ struct RouteGradientArgs {
     void* dlogits;             // [n, n_experts]
 };
 
-// 16 bytes, or one element, past the caches: a later kernel reads them (a million rows of 256: 226 us, 273 through them)
+// 16 bytes, or one element, past the caches: a later kernel reads them (a million rows of 256: 273 -> 226 us)
 template <typename T, bool VEC>
 __device__ __forceinline__ void store_chunk(T* to, const T* part) {
     typedef uint32_t Word __attribute__((ext_vector_type(4)));
@@ -331,21 +331,25 @@ __global__ void __launch_bounds__(256) k_route_gradient(RouteGradientArgs p) {
     if (i >= p.n) return;   // (whole rows leave; the others' lanes stay together)
     constexpr int epc = VEC ? 16 / (int)sizeof(T) : 1;
     int32_t expert[K];
-    float given[K], inner = 0.f;
+    float weight[K], given[K], inner = 0.f;
+#pragma unroll
+    for (int j = 0; j < K; ++j) {   // (all loads at once, no branches: their way is what a row takes)
+        const int64_t at = i * p.k + (j < p.k ? j : 0);
+        expert[j] = p.experts[at];
+        weight[j] = p.weights[at];
+        given[j] = p.dweights[at];
+    }
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-        expert[j] = -1;
-        given[j] = 0.f;
-        if (j >= p.k) continue;
-        expert[j] = p.experts[i * p.k + j];
-        if (expert[j] < 0) continue;
-        given[j] = p.dweights[i * p.k + j];
-        inner += p.weights[i * p.k + j] * given[j];
+        if (j >= p.k) expert[j] = -1;
+        weight[j] = expert[j] < 0 ? 0.f : weight[j];
+        given[j] = expert[j] < 0 ? 0.f : given[j];
+        inner += weight[j] * given[j];
     }
     T* out = (T*)p.dlogits + i * p.n_experts;
     if (p.normalize || expert[0] < 0) {
 #pragma unroll
-        for (int j = 0; j < K; ++j) given[j] = expert[j] < 0 ? 0.f : p.weights[i * p.k + (j < p.k ? j : 0)] * (given[j] - inner);
+        for (int j = 0; j < K; ++j) given[j] = weight[j] * (given[j] - inner);
         for (int32_t c = sub * epc; c < p.n_experts; c += LANES * epc) {
             T part[epc];
 #pragma unroll
