@@ -862,11 +862,11 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_gradient(GradientAr
     }
 }
 
-// The sums of the parts of long groups: a workgroup takes 1,024 elements of one
-constexpr int kPiece = 1024;
-template <typename O>
+// The sums of the parts of long groups, in the order of the parts, sixteen loads on their way at once: a workgroup takes 256 PER elements
+// of one group
+template <typename O, int PER>
 __global__ void __launch_bounds__(256) k_grouped_parts(GradientArgs p) {
-    const int64_t size = (int64_t)p.out * p.in, pieces = (size + kPiece - 1) / kPiece, block = block_number();
+    const int64_t size = (int64_t)p.out * p.in, pieces = (size + 256 * PER - 1) / (256 * PER), block = block_number();
     const int64_t number = block / pieces, piece = block - number * pieces;
     const int lane = threadIdx.x & 63;
     // long group `number`
@@ -894,27 +894,38 @@ __global__ void __launch_bounds__(256) k_grouped_parts(GradientArgs p) {
     }
     if (group < 0) return;
     const int32_t parts = parts_of(count, p.most);
-    const float* biases = p.part + p.slots * size;
+    // sums over the parts of the elements i, i + 256, ... of an array of `apart` a slot
+    const auto add = [&](const float* from, int64_t apart, int64_t i, float (&sum)[PER]) {
+        constexpr int batch = 16 / PER;
+#pragma unroll
+        for (int q = 0; q < PER; ++q) sum[q] = 0.f;
+        for (int32_t j0 = 0; j0 < parts; j0 += batch) {
+            float v[batch][PER];
+#pragma unroll
+            for (int j = 0; j < batch; ++j) {
+                const float* slot = from + slot_of(part_begin(begin, count, j0 + j < parts ? j0 + j : 0, parts), p.slot_bits) * apart;
+#pragma unroll
+                for (int q = 0; q < PER; ++q) v[j][q] = j0 + j < parts && i + q * 256 < apart ? slot[i + q * 256] : 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < batch; ++j)
+#pragma unroll
+                for (int q = 0; q < PER; ++q) sum[q] += v[j][q];
+        }
+    };
+    float sum[PER];
     if (p.db && piece == 0)
-        for (int32_t r = threadIdx.x; r < p.out; r += 256) {
-            float sum = 0.f;
-            for (int32_t j = 0; j < parts; ++j) sum += biases[slot_of(part_begin(begin, count, j, parts), p.slot_bits) * p.out + r];
-            p.db[(int64_t)group * p.out + r] = sum;
-        }
-    float sum[kPiece / 256] = {};
-    for (int32_t j = 0; j < parts; ++j) {
-        const float* from = p.part + slot_of(part_begin(begin, count, j, parts), p.slot_bits) * size;
+        for (int64_t r = threadIdx.x; r < p.out; r += 256 * PER) {
+            add(p.part + p.slots * size, p.out, r, sum);
 #pragma unroll
-        for (int q = 0; q < kPiece / 256; ++q) {
-            const int64_t i = piece * kPiece + q * 256 + threadIdx.x;
-            if (i < size) sum[q] += from[i];
+            for (int q = 0; q < PER; ++q)
+                if (r + q * 256 < p.out) p.db[(int64_t)group * p.out + r + q * 256] = sum[q];
         }
-    }
+    const int64_t i = piece * (256 * PER) + threadIdx.x;
+    add(p.part, size, i, sum);
 #pragma unroll
-    for (int q = 0; q < kPiece / 256; ++q) {
-        const int64_t i = piece * kPiece + q * 256 + threadIdx.x;
-        if (i < size) ((O*)p.dw)[(int64_t)group * size + i] = (O)sum[q];
-    }
+    for (int q = 0; q < PER; ++q)
+        if (i + q * 256 < size) ((O*)p.dw)[(int64_t)group * size + i + q * 256] = (O)sum[q];
 }
 
 }  // namespace nomad_grouped

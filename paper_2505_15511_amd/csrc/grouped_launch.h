@@ -75,8 +75,13 @@ void launch_gradient_type(const GradientArgs& p, const GradientPlan& plan, bool 
     } else if constexpr (sizeof(T) == 2) {
         launch_gradient<T, O, 256, 256, 4, 2, true, true>(p, units, st);
     }
-    if (p.slots > 0)   // (more than `most` rows in all: some group may be long)
-        hipLaunchKernelGGL((k_grouped_parts<O>), grid_of(p.rows / p.most * tiles_of((int64_t)p.in * p.out, kPiece)), dim3(256), 0, st, p);
+    if (p.slots > 0) {   // (more than `most` rows in all: some group may be long)
+        const int64_t size = (int64_t)p.in * p.out, groups = p.rows / p.most;
+        // few elements: one a lane, so that there are workgroups for all units (50 x 129, 400 parts: 18 us; four a lane 186, one part after
+        // the other); many: four (256 x 128 in 128 groups: 12 us, 61 with one)
+        if (size < 16384) hipLaunchKernelGGL((k_grouped_parts<O, 1>), grid_of(groups * tiles_of(size, 256)), dim3(256), 0, st, p);
+        else hipLaunchKernelGGL((k_grouped_parts<O, 4>), grid_of(groups * tiles_of(size, 1024)), dim3(256), 0, st, p);
+    }
 }
 
 }  // namespace nomad_grouped

@@ -47,11 +47,13 @@ inline GradientPlan plan_gradient(int64_t rows, int64_t groups, int64_t in, int6
     else if (small && in > 128 && out > 128 && large * groups >= units / 2) { plan.tile = kGradient256; plan.tiles = large; }
     else if (little * 16 < middle * 48) { plan.tile = kGradient64; plan.tiles = little; }   // a quarter less to compute, or more (40,022 rows, 50 x 129 in float32: 49 us, 78 in tiles of 128)
     else { plan.tile = kGradient128; plan.tiles = middle; }
-    // A quarter of a compute unit's share of the whole, so that the units end together (a group of 48,000 rows, 2,048 x 768: 2.1 ms,
-    // 2.5 with whole shares); but writing and reading a part's sums costs as much as about a thousand of its rows, so no
-    // shorter than 4,096 as long as that is no more than a share (800 rows a group, 512 x 768: 0.29 ms, 0.41 with quarters of one), nor than 256.
-    const int64_t share = rows * plan.tiles / units;
-    plan.most = (int32_t)std::min<int64_t>(std::max<int64_t>({256, share / 4, std::min<int64_t>(share, 4096)}), (int64_t)1 << 30);
+    // A quarter of a workgroup's share of the whole, so that they end together (groups of 8,192 rows, 2,048 x 768 in bfloat16: 2.1 ms, 2.5
+    // with whole shares).  But a part's sums are written and read once more: as many bytes as reading some rows, and no part has fewer
+    // than eight times those (256 x 256 in bfloat16: 4,096; groups of 800 rows, 512 x 768: 0.29 ms, 0.41 with quarters of a
+    // share) unless the share itself is less; nor fewer than 256, four stages of the products.
+    const int64_t a = plan.tile == kGradient256 ? 256 : plan.tile == kGradient64 ? 64 : 128, b = plan.tile == kGradient16 ? 16 : a;
+    const int64_t share = rows * plan.tiles / (units * (plan.tile == kGradient256 ? 1 : 2)), least = 8 * (a * b * 8) / ((a + b) * (small ? 2 : 4));
+    plan.most = (int32_t)std::min<int64_t>(std::max<int64_t>({256, share / 4, std::min(share, least)}), (int64_t)1 << 30);
     plan.slot_bits = 0;
     while ((int64_t)2 << plan.slot_bits <= plan.most / 2) ++plan.slot_bits;
     plan.slots = rows > plan.most ? (rows >> plan.slot_bits) + 1 : 0;

@@ -133,7 +133,8 @@ def test_routing_many_rows_against_torch():
 PRODUCTS = [(1, 1, 1, 1, F32, "ragged"), (3, 1, 50, 129, F32, "one"), (4, 300, 50, 129, F32, "ragged"), (2, 130, 7, 3, BF16, "ragged"), (5, 700, 64, 2, BF16, "ragged"),
             (8, 1000, 128, 256, BF16, "ragged"), (8, 5, 768, 96, F16, "ragged"), (3, 600, 129, 130, F16, "ragged"), (1, 513, 768, 72, BF16, "even"), (70, 900, 64, 40, F32, "ragged"),
             (5, 33_000, 72, 520, BF16, "ragged"), (130, 9_000, 264, 272, F16, "ragged"), (2, 20_000, 256, 136, BF16, "ragged"), (3, 9_000, 20, 12, F32, "one"),
-            (6, 400, 2, 260, F32, "ragged"), (4, 0, 16, 16, BF16, "empty"), (3, 64, 24, 24, BF16, "empty"), (2, 2100, 200, 264, BF16, "ragged"), (1030, 2000, 40, 24, F16, "ragged")]
+            (6, 400, 2, 260, F32, "ragged"), (4, 0, 16, 16, BF16, "empty"), (3, 64, 24, 24, BF16, "empty"), (2, 2100, 200, 264, BF16, "ragged"), (1030, 2000, 40, 24, F16, "ragged"),
+            (9000, 5000, 40, 24, F16, "ragged")]
 
 
 @pytest.mark.parametrize("groups,total,inner,out,dtype,kind", PRODUCTS)
