@@ -3,7 +3,8 @@
 //   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  p = (1 - lr wd) p - (lr / c1) m / (sqrt(v) / sqrt(c2) + eps)
 //
 // One pass over the elements, eight neighbouring ones a lane: bound by their bytes (28 an element in float32, 10 with 16-bit
-// parameters and 8-bit states), and with 8-bit states nearly as much by the arithmetic of decoding and encoding.
+// parameters and 8-bit states), and with 8-bit states nearly as much by the arithmetic of decoding and encoding: 97 M elements in
+// bfloat16 with 8-bit states take 202 us, 4.9 TB/s of the 5.4 of a large copy.
 //
 // 8 bits: blocks of 256 elements (the 32 lanes of half a wavefront) have one float32 scale s, their largest magnitude.
 // m = s (c / 127) |c / 127| and v = s (c / 255)^4: codes are denser near zero, where most of a block's averages are (v spans
@@ -21,7 +22,7 @@ constexpr int kTensors = 64;              // a launch: their addresses are its a
 constexpr int kThreads = 256, kPer = 8;   // lanes a workgroup, elements a lane
 constexpr int kChunk = kThreads * kPer;   // elements a workgroup takes at a time
 constexpr int kTurns = 4;                 // and how often, where there are enough for every compute unit: 2,048 elements are little beside
-                                          // the search for their tensor and the first load's way (97 M elements: 255 us, 260 taken once)
+                                          // the search for their tensor and the first load's way (97 M elements in 8 bits: 202 us, 207 taken once)
 constexpr int kBlock = 256;               // elements a scale
 constexpr int kLanes = kBlock / kPer;
 

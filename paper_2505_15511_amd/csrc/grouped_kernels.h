@@ -196,7 +196,7 @@ struct Source {
 
 // TILE rows (KC) or columns (not KC) by one stage of k, for NT threads.  PICKED: source rows anywhere (KC: a pointer each; otherwise
 // the numbers of 64 rows at a time in a register of the wavefront, the next 64 on their way).  ASYNC: loads go to LDS directly, whole
-// 16-byte chunks; otherwise through registers, element by element where a chunk is cut off.
+// 16-byte chunks; otherwise through registers, wherever rows begin and end.
 template <typename T, int TILE, bool KC, bool PICKED, int Q, bool ASYNC, int NT>
 struct Operand {
     static constexpr int kEpc = 16 / (int)sizeof(T);             // elements a chunk
@@ -274,6 +274,16 @@ struct Operand {
             now = (int32_t)src.row_at(next);
             next = entry(k0 + 64 + (tid & 63));
         }
+        if (!ASYNC && !KC && shorter()) {
+#pragma unroll
+            for (int it = 0; it < kPer; ++it) {
+                const T* from;
+                int elements;
+                chunk(it, tid, k0, from, elements);
+                held[ASYNC ? 0 : it] = has(it, tid) ? one_by_one(from, elements) : make_uint4(0, 0, 0, 0);
+            }
+            return;
+        }
 #pragma unroll
         for (int it = 0; it < kPer; ++it) {
             if (!has(it, tid)) continue;   // (kChunks is a multiple of 64: whole wavefronts)
@@ -286,22 +296,44 @@ struct Operand {
                                                  (__attribute__((address_space(3))) uint32_t*)(lds + it * NT + (tid & ~63)), 16, 0, 0);
             } else {
                 uint4 v = make_uint4(0, 0, 0, 0);
-                if (elements >= kEpc) {
-                    __builtin_memcpy(&v, from, 16);   // (aligned as an element is)
+                if (!KC) {
+                    if (elements > 0) __builtin_memcpy(&v, from - (elements < kEpc ? kEpc - elements : 0), 16);   // (aligned as an element is)
+                } else if (elements >= kEpc) {
+                    __builtin_memcpy(&v, from, 16);
                 } else if (elements > 0) {
-                    T part[kEpc] = {};
-#pragma unroll
-                    for (int i = 0; i < kEpc; ++i)
-                        if (i < elements) part[i] = from[i];
-                    __builtin_memcpy(&v, part, 16);
+                    v = one_by_one(from, elements);
                 }
                 held[ASYNC ? 0 : it] = v;
             }
         }
     }
-    // puts down what was asked for, where the loads did not
-    __device__ __forceinline__ void put(uint4* lds, int tid) const {
+    static __device__ __forceinline__ uint4 one_by_one(const T* from, int elements) {   // (fewer than a chunk)
+        T part[kEpc] = {};
+#pragma unroll
+        for (int i = 0; i < kEpc - 1; ++i)
+            if (i < elements) part[i] = from[i];
+        uint4 v;
+        __builtin_memcpy(&v, part, 16);
+        return v;
+    }
+    __device__ __forceinline__ bool shorter() const { return across + width < kEpc; }   // not KC: whole rows, than a chunk
+    // Puts down what was asked for, where the loads did not.  A chunk that is cut off: where k is contiguous that is in the last stage
+    // alone, and its elements were loaded one by one; columns are cut off in every row of k, and what is left of a chunk was loaded as the
+    // last 16 bytes of its row and moves to its beginning here (200,006 rows of float32, weights' gradient of 129 x 50: 102 us, 133 with
+    // elements one by one; products of 64 -> 129 the other way round: 80 us, 89 moved).
+    __device__ __forceinline__ void put(uint4* lds, int tid) {
         if (ASYNC) return;
+        if (!KC && width < TILE && !shorter()) {
+#pragma unroll
+            for (int it = 0; it < kPer; ++it) {
+                const int l = it * NT + tid, r = l / kCpr, c = (l % kCpr) ^ chunk_twist<T, TILE, KC, Q>(r);
+                const int over = (c + 1) * kEpc - width, bytes = (over > 0 && over < kEpc ? over : 0) * (int)sizeof(T);
+                uint4& v = held[ASYNC ? 0 : it];
+                if (bytes & 8) v = make_uint4(v.z, v.w, 0, 0);
+                if (bytes & 4) v = make_uint4(v.y, v.z, v.w, 0);
+                if (sizeof(T) == 2 && bytes & 2) v = make_uint4(v.x >> 16 | v.y << 16, v.y >> 16 | v.z << 16, v.z >> 16 | v.w << 16, v.w >> 16);
+            }
+        }
 #pragma unroll
         for (int it = 0; it < kPer; ++it)
             if (has(it, tid)) lds[it * NT + tid] = held[ASYNC ? 0 : it];
@@ -471,19 +503,26 @@ struct Rows16 {
             __builtin_memcpy(__builtin_assume_aligned(patch + row * kCols * (int)sizeof(X) + (((byte >> 4) ^ (row & kMask)) << 4) + (byte & 15), sizeof(part)), part, sizeof(part));
         }
     }
-    // rows 0 .. count - 1 of the 16, columns below `columns` from `to` on; whole: 16 aligned bytes at a time, otherwise one by one,
-    // neighbours by neighbouring lanes
+    // rows 0 .. count - 1 of the 16, columns below `columns` from `to` on, 16 bytes at a time; not whole: wherever rows begin, and one by
+    // one behind the last 16
     template <bool WHOLE>
     static __device__ __forceinline__ void send(const char* patch, X* to, int64_t stride, int count, int columns, int lane) {
         if (!WHOLE) {
-            constexpr int rows = kCols >= 64 ? 1 : 64 / kCols, across = kCols >= 64 ? kCols / 64 : 1;   // at a time, steps a row
+            constexpr int n = 16 / (int)sizeof(X);
 #pragma unroll
-            for (int r = 0; r < 16; r += rows)
+            for (int t = 0; t < 16 * kChunks; t += 64) {
+                const int at = t + lane, row = at / kChunks, chunk = at % kChunks, left = columns - chunk * n;
+                if ((16 * kChunks >= 64 || at < 16 * kChunks) && row < count && left > 0) {
+                    X part[n];
+                    __builtin_memcpy(part, __builtin_assume_aligned(patch + (row * kChunks + (chunk ^ (row & kMask))) * 16, 16), 16);
+                    X* at_row = to + row * stride + chunk * n;
+                    if (left >= n) __builtin_memcpy(at_row, part, 16);   // (aligned as an element is)
+                    else
 #pragma unroll
-                for (int c = 0; c < across; ++c) {
-                    const int row = r + (kCols >= 64 ? 0 : lane / kCols), col = kCols >= 64 ? 64 * c + lane : lane % kCols, byte = col * (int)sizeof(X);
-                    if (row < count && col < columns) to[row * stride + col] = *(const X*)(patch + row * kCols * (int)sizeof(X) + (((byte >> 4) ^ (row & kMask)) << 4) + (byte & 15));
+                        for (int j = 0; j < n - 1; ++j)
+                            if (j < left) at_row[j] = part[j];
                 }
+            }
             return;
         }
         typedef uint32_t Word __attribute__((ext_vector_type(4)));
@@ -504,9 +543,9 @@ struct Rows16 {
 //
 // What bounds it: the matrix cores, and what does not go on under them, a tile's activation and stores.  524,288 rows of 768 -> 2,048 in
 // bfloat16, gathered, with bias and SiLU: 2.0 ms, 830 TFLOP/s (a plain library product of that size 1.57 ms); without the SiLU 1.88;
-// 48 rows through 64 experts of that size 32 us, 6.3 TB/s of weights.
+// 48 rows through 64 experts of that size 30 us, 6.7 TB/s of weights.
 // LOADS, STORES: rows are made of whole aligned 16-byte chunks where they are read (straight to LDS), where they are written; otherwise
-// element by element at the ends.
+// through registers, and wherever rows begin and end: 200,006 rows of 50 -> 129 in float32 113 us, of 52 -> 132 81.
 template <typename T, typename O, int TA, int TB, int WA, int WB, bool W_KC, bool LOADS, bool STORES>
 __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_product(ProductArgs p) {
     typedef Tile<T, O, TA, TB, WA, WB, W_KC, false, true, true, LOADS> Work;
@@ -781,7 +820,7 @@ __device__ __forceinline__ void find_unit(const GradientArgs& p, Unit& u, int32_
 // dW = sum over the group's rows of dy^T x: tiles of TA columns of x and TB of dy.  The tiles of a part go to one XCD, side by side: they read
 // the same rows.  Workgroups stay and take every so many-th tile of their XCD, in turn from either end, as the parts get shorter.
 // Both operands are turned on their way out of LDS.  524,288 rows, 2,048 x 768 in bfloat16: 2.0 ms, 810 TFLOP/s; 200,006 rows in 256 groups,
-// 512 x 768: 0.29 ms, where rows and results alone are 0.15 at the rate of a large copy.
+// 512 x 768: 0.31 ms, where rows and results alone are 0.15 at the rate of a large copy.
 template <typename T, typename O, int TA, int TB, int WA, int WB, bool LOADS, bool STORES>
 __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_gradient(GradientArgs p) {
     typedef Tile<T, O, TA, TB, WA, WB, false, true, false, false, LOADS> Work;
