@@ -23,7 +23,7 @@ inline ProductTile plan_product(int64_t rows, int64_t groups, int64_t out, bool 
     if (w_kc && rows <= 16 * groups && row_tiles(128) * tiles_of(out, 128) < units) return kProductFew;
     if (out <= 16) return kProduct16;   // (131,072 rows of 256 -> 2 in float32: 44 us, 67 in tiles of 64 columns)
     // narrow tiles read x more often, and are right where wide ones would be empty: 129 columns are three of 64, not two of 128
-    // (200,006 rows of 50 -> 129 in float32: 118 us, 127 in tiles of 128)
+    // (200,006 rows of 50 -> 129 in float32, elements at the ends one by one on both sides: 118 us, 127 in tiles of 128; 113 now)
     if (out <= 64 || tiles_of(out, 64) * 64 * 9 < tiles_of(out, 128) * 128 * 8) return kProduct64;
     if (!small || out <= 128) return kProduct128;
     // large tiles where they are at least half full and there is one for every compute unit
@@ -42,10 +42,10 @@ struct GradientPlan {
 inline GradientPlan plan_gradient(int64_t rows, int64_t groups, int64_t in, int64_t out, bool small, int64_t units) {
     GradientPlan plan;
     const int64_t large = tiles_of(in, 256) * tiles_of(out, 256), middle = tiles_of(in, 128) * tiles_of(out, 128), little = tiles_of(in, 64) * tiles_of(out, 64);
-    // (131,072 rows, 2 x 256 in float32: 50 us, 100 in tiles of 64 x 64)
+    // (131,072 rows, 2 x 256 in float32: 58 us, 100 in tiles of 64 x 64)
     if (out <= 16 && in > 64) { plan.tile = kGradient16; plan.tiles = tiles_of(in, 128) * tiles_of(out, 16); }
     else if (small && in > 128 && out > 128 && large * groups >= units / 2) { plan.tile = kGradient256; plan.tiles = large; }
-    else if (little * 16 < middle * 48) { plan.tile = kGradient64; plan.tiles = little; }   // a quarter less to compute, or more (40,022 rows, 50 x 129 in float32: 42 us, 68 in tiles of 128)
+    else if (little * 16 < middle * 48) { plan.tile = kGradient64; plan.tiles = little; }   // a quarter less to compute, or more (40,022 rows, 50 x 129 in float32, elements at the ends one by one on both sides: 42 us, 68 in tiles of 128; 34 now)
     else { plan.tile = kGradient128; plan.tiles = middle; }
     // A quarter of a workgroup's share of the whole, so that they end together (groups of 8,192 rows, 2,048 x 768 in bfloat16: 2.1 ms, 2.5
     // with whole shares).  But a part's sums are written and read once more: as many bytes as reading some rows, and no part has fewer
