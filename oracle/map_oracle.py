@@ -156,3 +156,24 @@ def decode_first(codes, scales):
 
 def decode_second(codes, scales):
     return (codes.astype(np.float64) / 255.0) ** 4 * np.repeat(scales.astype(np.float64), BLOCK)[:codes.size]
+
+
+def _scaled(magnitude, most):
+    """(scales of the blocks, every magnitude in units where its block's scale is `most`)."""
+    scales = np.array([magnitude[b:b + BLOCK].max() for b in range(0, magnitude.size, BLOCK)])
+    scales[scales < 2.0 ** -126] = 0.0
+    each = np.repeat(scales, BLOCK)[:magnitude.size]
+    return scales, np.where(each > 0, magnitude / np.where(each > 0, each, 1.0) * most, 0.0)
+
+
+def encode_first(m):
+    """(codes, scales, t) with (c - 1/2)^2 <= t < (c + 1/2)^2; codes carry the sign."""
+    scales, t = _scaled(np.abs(m), 127.0 ** 2)
+    return np.sign(m) * np.floor(np.sqrt(t) + 0.5), scales, t
+
+
+def encode_second(v):
+    """(codes, scales, t), to the fourth power; a code is at least 1 where v > 0."""
+    scales, t = _scaled(v, 255.0 ** 4)
+    codes = np.floor(t ** 0.25 + 0.5)
+    return np.where(t > 0, np.maximum(codes, 1.0), 0.0), scales, t

@@ -9,7 +9,8 @@
 // 8 bits: blocks of 256 elements (the 32 lanes of half a wavefront) have one float32 scale s, their largest magnitude.
 // m = s (c / 127) |c / 127| and v = s (c / 255)^4: codes are denser near zero, where most of a block's averages are (v spans
 // 2.4e-10 of its block's largest; a linear code would round the small ones to zero and their steps to m / eps).  A code is the
-// whole number c with (c - 1/2)^2 <= t < (c + 1/2)^2 for t = |m| (127^2 / s), to the fourth power for v with t = v (255^4 / s);
+// whole number c with (c - 1/2)^2 <= t < (c + 1/2)^2 for t = |m| (127^2 / s), to the fourth power for v with t = v (255^4 / s), for
+// any scale of at least 2^-126 (small ones are multiplied by a power of two first, which changes no t);
 // v's is 0 only where v is.  The averages round every operation once, without fused ones, and borders are compared in float32: the
 // codes are the same whatever computes them.  The step itself uses the hardware's reciprocal and root (one unit in the last place each).
 #pragma once
@@ -67,6 +68,9 @@ __device__ __forceinline__ void store8(T* to, int n, const T (&v)[kPer]) {
             if (i < n) to[i] = v[i];
     }
 }
+
+// scales below kSmall are lifted by kLift: 255^4 / kSmall is finite, and a lifted scale is a normal number far from either end
+constexpr float kSmall = 0x1p-90f, kLift = 0x1p64f;
 
 __device__ __forceinline__ float decode_first(int c, float s) {
 #pragma clang fp contract(off)
@@ -164,7 +168,12 @@ __device__ __forceinline__ void step8(const Tensor& t, const Scalars& s, int64_t
             v_most = vb > v_most ? vb : v_most;
         }
         const float ms = scale_of(block_most(m_most)), vs = scale_of(block_most(v_most));
-        const float mf = ms == 0.f ? 0.f : 16129.f / ms, vf = vs == 0.f ? 0.f : 4228250625.f / vs;
+        // 127^2 / s and 255^4 / s have to be numbers: small averages and their scale are first multiplied by the same power of two
+        const float m_lift = ms < kSmall ? kLift : 1.f, v_lift = vs < kSmall ? kLift : 1.f;
+        const float mf = ms == 0.f ? 0.f : 16129.f / (ms * m_lift), vf = vs == 0.f ? 0.f : 4228250625.f / (vs * v_lift);
+        if (__any(m_lift != 1.f || v_lift != 1.f))
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) { m[i] *= m_lift; v[i] *= v_lift; }
         float off_first = 0.f, off_second = 0.f, mr[kPer], vr[kPer];
 #pragma unroll
         for (int i = 0; i < kPer; ++i) { mr[i] = root_first(m[i], mf, off_first); vr[i] = root_second(v[i], vf, off_second); }

@@ -364,6 +364,39 @@ def test_adamw_8_bits_zeros_and_values_that_are_not_finite():
     assert (v.scales == 0).all() and (m.codes == 127).all() and torch.isfinite(q).all()
 
 
+#: scales of a block around and below the ones whose quotients 127^2 / s and 255^4 / s are no float32 numbers (4.7e-35, 1.24e-29)
+SMALL_SCALES = [1.2e-38, 1e-37, 1e-36, 4e-35, 5e-35, 1e-33, 1e-30, 1.2e-29, 1.3e-29, 8e-28, 9e-28, 1e-20]
+
+
+@pytest.mark.parametrize("which", ["first", "second"])
+def test_adamw_8_bits_small_scales(which):
+    """One block a scale, its averages four decades and both signs: codes are those of the borders at every scale.  An average is the
+    sum and product of a few float32 numbers: good to some 2^-24 of itself and some 2^-149, its distance to a border likewise."""
+    note(f"adamw 8 small scales of the {which} averages")
+    rng = np.random.default_rng(23)
+    beta1, beta2 = 0.5, 0.75                                           # (powers of two: the products add no rounding of their own)
+    g = np.concatenate([(s / 0.5 if which == "first" else np.sqrt(s / 0.25)) * np.where(np.arange(256) == 0, 1.0, 10.0 ** rng.uniform(-4, 0, 256)) * rng.choice([-1.0, 1.0], 256)
+                        for s in SMALL_SCALES]).astype(np.float32)
+    p, grad = torch.ones(g.size, device="cuda"), torch.from_numpy(g).cuda()
+    m, v = nomad.adamw_state(p, 8)
+    nomad.adamw_step([p], [grad], [m], [v], 1, lr=0.1, betas=(beta1, beta2), weight_decay=0.0)
+    g = g.astype(np.float64)
+    state, average, encode, most, power = (m, 0.5 * g, mo.encode_first, 127, 2) if which == "first" else (v, 0.25 * g * g, mo.encode_second, 255, 4)
+    codes, scales = state.codes.cpu().numpy().astype(np.float64), state.scales.cpu().numpy().astype(np.float64)
+    want, want_scales, t = encode(average)
+    assert np.all(np.abs(scales - want_scales) <= 8 * U32 * want_scales + 2.0 ** -147)
+    slack = 64 * U32 * t + 2.0 ** -147 * most ** power / np.repeat(want_scales, 256)
+    a = np.abs(codes)
+    assert np.all(t - slack < (a + 0.5) ** power)
+    assert np.all((t + slack >= np.maximum(a - 0.5, 0.0) ** power) | ((power == 4) & (a == 1)))
+    assert np.all((np.sign(codes) == np.sign(average)) | (codes == 0))
+    assert np.mean(codes == want) > 0.95 and np.array_equal(codes.reshape(-1, 256)[:, 0], want.reshape(-1, 256)[:, 0])
+    # and they decode to the average, within half a code's step
+    shown = host(nomad.adamw_state_values([state])[0])
+    step = np.repeat(want_scales, 256) * ((a + 0.5) ** power - np.maximum(a - 0.5, 0.0) ** power) / most ** power
+    assert np.all(np.abs(shown - average) <= step * 1.001 + 2.0 ** -147)
+
+
 # ---- streams and refusals
 
 

@@ -77,3 +77,21 @@ def test_adamw_first_step_is_the_sign():
     p, m, v = mo.adamw(np.array([1.0, -2.0]), np.array([0.5, -3.0]), np.zeros(2), np.zeros(2), 1, 0.1, 0.9, 0.999, 0.0, 0.0)
     assert np.allclose(p, [0.9, -1.9]) and np.allclose(m, [0.05, -0.3]) and np.allclose(v, [2.5e-4, 9e-3])
     assert np.allclose(mo.adamw(np.array([1.0]), np.zeros(1), np.zeros(1), np.zeros(1), 1, 0.1, 0.9, 0.999, 1e-8, 0.5)[0], 0.95)
+
+
+def test_codes_of_8_bits_are_the_nearest_at_any_scale():
+    """Every code lies between its borders, and the value it stands for within half a step, for scales from one to the smallest."""
+    rng = np.random.default_rng(5)
+    for top in (1.0, 1e-20, 1e-28, 1.2e-29, 1e-33, 4e-35, 1e-37, 2.0 ** -126):
+        x = rng.normal(size=700) * 10.0 ** rng.uniform(-6, 0, size=700)
+        x *= top / np.abs(x).max()
+        x[[0, 300, 600]] = top, -top, top                     # every block has that scale
+        for encode, decode, v, most, power in ((mo.encode_first, mo.decode_first, x, 127, 2), (mo.encode_second, mo.decode_second, np.abs(x), 255, 4)):
+            codes, scales, t = encode(v)
+            assert all(scales[b] == np.abs(v[256 * b:256 * b + 256]).max() for b in range(3)) and np.abs(codes).max() == most
+            a = np.abs(codes)
+            assert np.all(t < (a + 0.5) ** power * (1 + 1e-12)) and np.all((t >= np.maximum(a - 0.5, 0.0) ** power * (1 - 1e-12)) | ((power == 4) & (a == 1)))
+            value = decode(codes, scales)
+            assert np.all(np.abs(np.abs(value) - np.abs(v)) <= top * ((a + 0.5) ** power - np.maximum(a - 0.5, 0.0) ** power) / most ** power)
+            assert np.all((np.sign(value) == np.sign(v)) | (codes == 0))
+    assert (mo.encode_first(np.full(10, 1e-38))[0] == 0).all() and (mo.encode_second(np.zeros(10))[0] == 0).all()
