@@ -666,8 +666,9 @@ int nomad_combine_gradient(const void* dy, int32_t dtype, int64_t dy_stride, con
  * (p fp32) any.  bits = 32: m and v fp32 [n].  bits = 8: m int8 [n] and v uint8 [n] codes with a scale (fp32) per block of
  * NOMAD_ADAMW_BLOCK consecutive elements in m_scale and v_scale: m = s (c / 127) |c / 127|, v = s (c / 255)^4, s the largest
  * magnitude of the block (0 where that is below 2^-126); c is the whole number with (c - 1/2)^2 <= |m| 127^2 / s < (c + 1/2)^2, to
- * the fourth power with 255 for v, whose code is at least 1 where v > 0.  A gradient that is NaN or infinite makes its block's
- * averages NaN.  All zeros is the state before the first step (step = 1).  Tensors and states must not overlap.
+ * the fourth power with 255 for v, whose code is at least 1 where v > 0.  An average that is NaN or infinite (its gradient is,
+ * or its gradient's square passes float32) makes that average of its whole block NaN.  All zeros is the state before the first
+ * step (step = 1).  Tensors and states must not overlap.
  */
 #define NOMAD_ADAMW_BLOCK 256
 typedef struct {

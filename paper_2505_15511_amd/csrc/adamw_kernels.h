@@ -92,9 +92,9 @@ __device__ __forceinline__ uint32_t block_most(uint32_t bits) {
     }
     return bits;
 }
-// (a NaN or an infinity makes the scale one, and so the block's values NaN: they do not disappear)
+// (a NaN or an infinity makes the scale NaN, and so the block's values: they do not disappear)
 __device__ __forceinline__ float scale_of(uint32_t bits) {
-    return bits < 0x00800000u ? 0.f : __uint_as_float(bits);
+    return bits < 0x00800000u ? 0.f : __uint_as_float(bits < 0x7f800000u ? bits : 0x7fc00000u);
 }
 // Roots by the hardware, whose last place may be off by one: `off` collects how far they lie from their whole numbers, and where none
 // is nearer to a border than that error reaches (kSure: 128 2^-23, and one and a half times that of 255 for the fourth root

@@ -397,6 +397,19 @@ def test_adamw_8_bits_small_scales(which):
     assert np.all(np.abs(shown - average) <= step * 1.001 + 2.0 ** -147)
 
 
+def test_adamw_8_bits_averages_that_are_not_finite():
+    """A block with an average that is NaN or infinite is NaN, of the first averages and of the second; its neighbours are not."""
+    note("adamw 8 averages that are not finite")
+    g = torch.full((1280,), 0.5, device="cuda")
+    g[300], g[600], g[900] = float("nan"), float("inf"), 1e25          # (the square of the last one passes float32)
+    p = torch.ones(1280, device="cuda")
+    m, v = nomad.adamw_state(p, 8)
+    nomad.adamw_step([p], [g], [m], [v], 1, lr=0.1, weight_decay=0.0)
+    first, second = nomad.adamw_state_values([m])[0].view(5, 256), nomad.adamw_state_values([v])[0].view(5, 256)
+    assert first[1:3].isnan().all() and first[[0, 3, 4]].isfinite().all()
+    assert second[1:4].isnan().all() and second[[0, 4]].isfinite().all()
+
+
 # ---- streams and refusals
 
 
