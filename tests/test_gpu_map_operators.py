@@ -410,6 +410,25 @@ def test_adamw_8_bits_averages_that_are_not_finite():
     assert second[1:4].isnan().all() and second[[0, 4]].isfinite().all()
 
 
+@pytest.mark.parametrize("eps", [1e-8, 1e-30, 0.0])
+@pytest.mark.parametrize("bits,dtype", [(32, F32), (8, F32), (32, BF16), (8, BF16)])
+def test_adamw_steps_of_small_gradients(eps, bits, dtype):
+    """The step from the averages that the state shows, down to the smallest v that is not zero: from zero a parameter becomes minus
+    its step, which takes half a dozen roundings, the hardware's reciprocal and root among them."""
+    note(f"adamw small gradients eps={eps} bits={bits} {dtype}")
+    g = torch.logspace(-20.5, 2, 4096, device="cuda", dtype=torch.float64).float()
+    g[1::2] *= -1.0
+    p = torch.zeros(4096, device="cuda", dtype=dtype)
+    m, v = nomad.adamw_state(p, bits)
+    nomad.adamw_step([p], [g], [m], [v], 1, lr=0.25, betas=(0.5, 0.75), eps=eps, weight_decay=0.0)
+    first = 0.5 * host(g)                                              # exact: a power of two
+    d2 = (host(g).astype(np.float32) * host(g).astype(np.float32)).astype(np.float32)
+    second = (d2 * np.float32(0.25)).astype(np.float64)                # as float32 holds it, denormal numbers too
+    assert (second > 0).all() and (bits == 8 or np.array_equal(host(v), second))
+    want = -0.25 * (first / 0.5) / (np.sqrt(second / 0.25) + eps)
+    assert np.all(np.abs(host(p) - want) <= (16 * U32 + UNIT[dtype]) * np.abs(want))
+
+
 # ---- streams and refusals
 
 
