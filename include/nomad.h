@@ -669,6 +669,12 @@ int nomad_combine_gradient(const void* dy, int32_t dtype, int64_t dy_stride, con
  * the fourth power with 255 for v, whose code is at least 1 where v > 0.  An average that is NaN or infinite (its gradient is,
  * or its gradient's square passes float32) makes that average of its whole block NaN.  All zeros is the state before the first
  * step (step = 1).  Tensors and states must not overlap.
+ * Nearest codes (dither = 0) stay where they are while a step changes an average by less than half the way to the next code.  A second
+ * average then does not decay against its block's largest where 1 - beta2 is below 0.8 % (or more, for codes below 255), so that an
+ * element whose gradients have become small keeps a v, and with it steps, of the large ones: use them where beta2 is 0.99 or less, or
+ * blocks' elements are alike.  dither = 1 draws the border between two codes evenly between the values they stand for (c^2 + u ((c + 1)^2
+ * - c^2), fourth powers for v), u in (0, 1) from the step and the element's place in its tensor: the values that codes stand for are then
+ * the averages in expectation at any beta, and a call gives the same codes whenever it is made with the same arguments.
  */
 #define NOMAD_ADAMW_BLOCK 256
 typedef struct {
@@ -689,6 +695,7 @@ typedef struct {
   const float* grad_scale;
   void* stream;
   int32_t device;
+  int64_t dither; /* bits = 8: 0 nearest codes, 1 dithered ones (struct_size may end before it: 0) */
 } nomad_adamw_options;
 int nomad_adamw_step(const nomad_adamw_tensor* tensors, int32_t count, const nomad_adamw_options* options);
 

@@ -166,14 +166,42 @@ def _scaled(magnitude, most):
     return scales, np.where(each > 0, magnitude / np.where(each > 0, each, 1.0) * most, 0.0)
 
 
-def encode_first(m):
-    """(codes, scales, t) with (c - 1/2)^2 <= t < (c + 1/2)^2; codes carry the sign."""
+def _codes(t, power, most, u):
+    """The nearest codes, or dithered ones: border between c and c + 1 at c^p + u ((c + 1)^p - c^p)."""
+    if u is None:
+        return np.floor(t ** (1.0 / power) + 0.5)
+    c = np.floor(t ** (1.0 / power))
+    return np.minimum(c + (t >= c ** power + u * ((c + 1.0) ** power - c ** power)), most)
+
+
+def encode_first(m, u=None):
+    """(codes, scales, t) with (c - 1/2)^2 <= t < (c + 1/2)^2, or dithered with u; codes carry the sign."""
     scales, t = _scaled(np.abs(m), 127.0 ** 2)
-    return np.sign(m) * np.floor(np.sqrt(t) + 0.5), scales, t
+    return np.sign(m) * _codes(t, 2, 127, u), scales, t
 
 
-def encode_second(v):
+def philox(counter, key):
+    """Philox4x32 with 10 rounds (Salmon et al., SC'11): counter [.., 4] and key (two words) as unsigned 32-bit numbers."""
+    c, (k0, k1), low = np.asarray(counter, dtype=np.uint64), (int(k) for k in key), np.uint64(0xFFFFFFFF)
+    c = [c[..., i].copy() for i in range(4)]
+    for r in range(10):
+        p0, p1 = c[0] * np.uint64(0xD2511F53), c[2] * np.uint64(0xCD9E8D57)
+        c = [(p1 >> np.uint64(32)) ^ c[1] ^ np.uint64((k0 + r * 0x9E3779B9) & 0xFFFFFFFF), p1 & low,
+             (p0 >> np.uint64(32)) ^ c[3] ^ np.uint64((k1 + r * 0xBB67AE85) & 0xFFFFFFFF), p0 & low]
+    return np.stack(c, -1)
+
+
+def draws(n, step, second):
+    """u of every element of a tensor: eight of 16 bits a call, the low half of a word first."""
+    eighth = np.arange(-(-n // 8))
+    counter = np.stack([eighth & 0xFFFFFFFF, eighth >> 32, np.full_like(eighth, int(second)), np.zeros_like(eighth)], -1)
+    words = philox(counter, (step & 0xFFFFFFFF, step >> 32))
+    halves = np.stack([words & np.uint64(0xFFFF), words >> np.uint64(16)], -1).reshape(-1)
+    return (halves[:n].astype(np.float64) + 0.5) / 65536.0
+
+
+def encode_second(v, u=None):
     """(codes, scales, t), to the fourth power; a code is at least 1 where v > 0."""
     scales, t = _scaled(v, 255.0 ** 4)
-    codes = np.floor(t ** 0.25 + 0.5)
+    codes = _codes(t, 4, 255, u)
     return np.where(t > 0, np.maximum(codes, 1.0), 0.0), scales, t

@@ -52,7 +52,7 @@ POOL_PICKS16, POOL_DISTINCT, POOL_STRATIFIED = 0, 1, 2
 GROUPED_PRODUCT_ARGS = struct.Struct("@I7i2q3Pq" "P3q" "PqPqPqPq" "Pi4x")
 GROUPED_GRADIENT_ARGS = struct.Struct("@I6i4x2q2P" "PqPq" "PP" "Pq" "Pi4x")
 ADAMW_TENSOR = struct.Struct("@6Pq2i")
-ADAMW_OPTIONS = struct.Struct("@Iiq5dPPi4x")
+ADAMW_OPTIONS = struct.Struct("@Iiq5dPPi4xq")
 
 
 class NomadError(RuntimeError):

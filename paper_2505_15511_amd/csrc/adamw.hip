@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <cstddef>
 
 #include "adamw_kernels.h"
 #include "host_util.h"
@@ -13,10 +14,11 @@ namespace {
 
 // launches, each with the addresses of up to kTensors tensors among its arguments
 template <typename P, typename G>
-void launch(const Batch& b, bool eight, hipStream_t st) {
+void launch(const Batch& b, bool eight, bool dither, hipStream_t st) {
     const dim3 grid(b.first[b.count]), block(kThreads);
-    if (eight) hipLaunchKernelGGL((k_adamw<P, G, true>), grid, block, 0, st, b);
-    else hipLaunchKernelGGL((k_adamw<P, G, false>), grid, block, 0, st, b);
+    if (eight && dither) hipLaunchKernelGGL((k_adamw<P, G, true, true>), grid, block, 0, st, b);
+    else if (eight) hipLaunchKernelGGL((k_adamw<P, G, true, false>), grid, block, 0, st, b);
+    else hipLaunchKernelGGL((k_adamw<P, G, false, false>), grid, block, 0, st, b);
 }
 
 int kind_of(int32_t p, int32_t g) {   // -1: no such step
@@ -26,15 +28,15 @@ int kind_of(int32_t p, int32_t g) {   // -1: no such step
     return -1;
 }
 
-void launch_kind(int kind, const Batch& b, bool eight, hipStream_t st) {
+void launch_kind(int kind, const Batch& b, bool eight, bool dither, hipStream_t st) {
     switch (kind) {
-        case 0: launch<float, float>(b, eight, st); break;
-        case 1: launch<float, __bf16>(b, eight, st); break;
-        case 2: launch<float, _Float16>(b, eight, st); break;
-        case 3: launch<__bf16, __bf16>(b, eight, st); break;
-        case 4: launch<__bf16, float>(b, eight, st); break;
-        case 5: launch<_Float16, _Float16>(b, eight, st); break;
-        default: launch<_Float16, float>(b, eight, st); break;
+        case 0: launch<float, float>(b, eight, dither, st); break;
+        case 1: launch<float, __bf16>(b, eight, dither, st); break;
+        case 2: launch<float, _Float16>(b, eight, dither, st); break;
+        case 3: launch<__bf16, __bf16>(b, eight, dither, st); break;
+        case 4: launch<__bf16, float>(b, eight, dither, st); break;
+        case 5: launch<_Float16, _Float16>(b, eight, dither, st); break;
+        default: launch<_Float16, float>(b, eight, dither, st); break;
     }
 }
 
@@ -48,9 +50,11 @@ constexpr int64_t kManyElements = (int64_t)256 * 8 * kChunk * kTurns;
 
 #pragma GCC visibility push(default)
 extern "C" int nomad_adamw_step(const nomad_adamw_tensor* tensors, int32_t count, const nomad_adamw_options* options) {
-    if (!options || options->struct_size != sizeof(nomad_adamw_options) || count < 0 || (count > 0 && !tensors)) return NOMAD_E_INVALID_ARG;
+    constexpr size_t shorter = offsetof(nomad_adamw_options, dither);   // options without it: nearest codes
+    if (!options || (options->struct_size != sizeof(nomad_adamw_options) && options->struct_size != shorter) || count < 0 || (count > 0 && !tensors)) return NOMAD_E_INVALID_ARG;
     const nomad_adamw_options& o = *options;
-    if ((o.bits != 8 && o.bits != 32) || o.step < 1 || o.device < 0) return NOMAD_E_INVALID_ARG;
+    const bool dither = o.struct_size != shorter && o.dither != 0;
+    if ((dither && (o.dither != 1 || o.bits != 8)) || (o.bits != 8 && o.bits != 32) || o.step < 1 || o.device < 0) return NOMAD_E_INVALID_ARG;
     if (!std::isfinite(o.lr) || !std::isfinite(o.weight_decay) || !(o.eps >= 0.0) || !std::isfinite(o.eps) || !(o.beta1 >= 0.0 && o.beta1 < 1.0) ||
         !(o.beta2 >= 0.0 && o.beta2 < 1.0))
         return NOMAD_E_INVALID_ARG;
@@ -73,6 +77,8 @@ extern "C" int nomad_adamw_step(const nomad_adamw_tensor* tensors, int32_t count
     b.s.c2 = (float)(1.0 - o.beta2);
     b.s.root = (float)(1.0 / std::sqrt(1.0 - std::pow(o.beta2, (double)o.step)));
     b.s.eps = (float)o.eps;
+    b.s.step_low = (uint32_t)o.step;
+    b.s.step_high = (uint32_t)((uint64_t)o.step >> 32);
     b.s.grad_scale = o.grad_scale;
     int64_t total = 0;
     for (int32_t i = 0; i < count; ++i) total += tensors[i].n;
@@ -81,7 +87,7 @@ extern "C" int nomad_adamw_step(const nomad_adamw_tensor* tensors, int32_t count
         b.count = 0;
         b.first[0] = 0;
         const auto flush = [&]() {
-            if (b.count > 0) launch_kind(kind, b, o.bits == 8, st);
+            if (b.count > 0) launch_kind(kind, b, o.bits == 8, dither, st);
             b.count = 0;
         };
         for (int32_t i = 0; i < count; ++i) {

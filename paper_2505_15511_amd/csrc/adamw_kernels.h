@@ -16,9 +16,18 @@
 // states of 8 the hardware's root and reciprocal stand in (one unit in the last place each, 2^-15 and less of what the parameter's own
 // rounding is; 97 M elements 240 us, 303 with the others, which cost nothing where more bytes move), and not for denormal numbers,
 // which that root takes for zero.
+//
+// Nearest codes hold an average where it is as long as a step changes it by less than half the way to the next code: v falls only
+// with its block's largest where 1 - beta2 is below 0.8 % (c = 255; more below), and rises on gradients far above its own.  Dithered
+// codes are right on average instead: the border between c and c + 1 lies at c^2 + u ((c + 1)^2 - c^2) (fourth powers for v), u drawn
+// evenly from (0, 1) for every element and step, so that the value that a code stands for is the average in expectation, and so are all
+// that follow from it.  u: 16 bits of Philox(counter = (element / 8, 0 for m or 1 for v), key = step); nothing is kept for it.  97 M elements
+// in bfloat16 302 us against 240 with nearest codes.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include "philox.h"
 
 namespace nomad_adamw {
 
@@ -41,6 +50,7 @@ struct Tensor {
 };
 struct Scalars {
     float keep, rate, b1, c1, b2, c2, root, eps;
+    uint32_t step_low, step_high;
     const float* grad_scale;   // NULL: 1
 };
 struct Batch {
@@ -132,7 +142,29 @@ __device__ __forceinline__ float border_second(float c, float v, float factor) {
 }
 
 constexpr float kRootNormal = 0x1p-96f;   // far enough above the smallest normal number
-template <typename P, typename G, bool EIGHT, bool WHOLE>
+// eight numbers of (0, 1), 16 bits each, for elements at .. at + 7
+__device__ __forceinline__ void draw8(int64_t at, uint32_t which, const Scalars& s, float (&u)[kPer]) {
+    uint32_t words[4];
+    const uint64_t eighth = (uint64_t)at / kPer;
+    philox4x32_10((uint32_t)eighth, (uint32_t)(eighth >> 32), which, 0u, s.step_low, s.step_high, words);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) u[i] = ((float)(words[i / 2] >> i % 2 * 16 & 0xffffu) + 0.5f) * 0x1p-16f;
+}
+// (a t within a rounding of a whole number's power may have that number or the one below for c: the border is next to it either way.
+// fminf makes a NaN, whose scale is one, the largest code)
+__device__ __forceinline__ float drawn_first(float m, float factor, float u) {
+    const float t = fabsf(m) * factor, c = fminf(floorf(__builtin_amdgcn_sqrtf(t)), 127.f);
+    return fminf(c + (t >= c * c + u * (2.f * c + 1.f) ? 1.f : 0.f), 127.f);
+}
+__device__ __forceinline__ float drawn_second(float v, float factor, float u) {
+    const float t = v * factor, c = fminf(floorf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(t))), 255.f);
+    float low = c * c, up = (c + 1.f) * (c + 1.f);
+    low = low * low;
+    up = up * up;
+    return fminf(c + (t >= low + u * (up - low) ? 1.f : 0.f), 255.f);
+}
+
+template <typename P, typename G, bool EIGHT, bool DITHER, bool WHOLE>
 __device__ __forceinline__ void step8(const Tensor& t, const Scalars& s, int64_t at, int n) {
 #pragma clang fp contract(off)
     P p[kPer];
@@ -186,12 +218,23 @@ __device__ __forceinline__ void step8(const Tensor& t, const Scalars& s, int64_t
         if (__any(m_lift != 1.f || v_lift != 1.f))
 #pragma unroll
             for (int i = 0; i < kPer; ++i) { m[i] *= m_lift; v[i] *= v_lift; }
-        float off_first = 0.f, off_second = 0.f, mr[kPer], vr[kPer];
+        float mr[kPer], vr[kPer];
+        if (DITHER) {
+            float u[kPer];
+            draw8(at, 0u, s, u);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) { mr[i] = root_first(m[i], mf, off_first); vr[i] = root_second(v[i], vf, off_second); }
-        if (__any(off_first > kSureFirst || off_second > kSureSecond))
+            for (int i = 0; i < kPer; ++i) mr[i] = drawn_first(m[i], mf, u[i]);
+            draw8(at, 1u, s, u);
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) { mr[i] = border_first(mr[i], m[i], mf); vr[i] = border_second(vr[i], v[i], vf); }
+            for (int i = 0; i < kPer; ++i) vr[i] = drawn_second(v[i], vf, u[i]);
+        } else {
+            float off_first = 0.f, off_second = 0.f;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) { mr[i] = root_first(m[i], mf, off_first); vr[i] = root_second(v[i], vf, off_second); }
+            if (__any(off_first > kSureFirst || off_second > kSureSecond))
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) { mr[i] = border_first(mr[i], m[i], mf); vr[i] = border_second(vr[i], v[i], vf); }
+        }
         const float least = vs > 0.f ? 0.f : __builtin_inff();   // what v is above where its code is at least 1
         int8_t mc[kPer];
         uint8_t vc[kPer];
@@ -211,7 +254,7 @@ __device__ __forceinline__ void step8(const Tensor& t, const Scalars& s, int64_t
 
 __device__ __forceinline__ bool aligned(const void* p, uintptr_t bytes) { return (uintptr_t)p % bytes == 0; }
 
-template <typename P, typename G, bool EIGHT>
+template <typename P, typename G, bool EIGHT, bool DITHER>
 __global__ void __launch_bounds__(kThreads) k_adamw(Batch b) {
     int lo = 0, hi = b.count;   // the tensor of this workgroup
     while (hi - lo > 1) {
@@ -225,8 +268,8 @@ __global__ void __launch_bounds__(kThreads) k_adamw(Batch b) {
     int64_t first = (int64_t)(blockIdx.x - b.first[lo]) * b.turns * kChunk;
     for (int turn = 0; turn < b.turns && first < t.n; ++turn, first += kChunk) {
         const int64_t at = first + (int64_t)threadIdx.x * kPer;
-        if (borders && first + kChunk <= t.n) step8<P, G, EIGHT, true>(t, b.s, at, kPer);
-        else step8<P, G, EIGHT, false>(t, b.s, at, (int)(t.n - at > kPer ? kPer : t.n - at));   // (every lane stays: the block's largest is found by all)
+        if (borders && first + kChunk <= t.n) step8<P, G, EIGHT, DITHER, true>(t, b.s, at, kPer);
+        else step8<P, G, EIGHT, DITHER, false>(t, b.s, at, (int)(t.n - at > kPer ? kPer : t.n - at));   // (every lane stays: the block's largest is found by all)
     }
 }
 

@@ -290,9 +290,10 @@ def adamw_state(param, bits=32):
     return tuple(State8(torch.zeros(n, dtype=d, device=param.device), torch.zeros(blocks, dtype=torch.float32, device=param.device)) for d in (torch.int8, torch.uint8))
 
 
-def adamw_step(params, grads, first, second, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_scale=None, stream=None):
+def adamw_step(params, grads, first, second, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_scale=None, dither=False, stream=None):
     """nomad_adamw_step: one step, in place, over all of the tensors at once.  first and second: the averages of `adamw_state`
-    (all in 32 bits, or all in 8); step counts from 1; grad_scale: None or a float32 tensor of one element on the GPU."""
+    (all in 32 bits, or all in 8); step counts from 1; grad_scale: None or a float32 tensor of one element on the GPU.  dither, for
+    averages in 8 bits: codes that are right on average instead of the nearest, which a beta2 above 0.99 needs to forget."""
     params, grads, first, second = list(params), list(grads), list(first), list(second)
     if not len(params) == len(grads) == len(first) == len(second):
         raise ValueError("params, grads, first and second must be lists of the same length")
@@ -300,6 +301,8 @@ def adamw_step(params, grads, first, second, step, lr=1e-3, betas=(0.9, 0.999), 
         return
     eight = not isinstance(first[0], torch.Tensor)
     device = params[0].device
+    if dither and not eight:
+        raise ValueError("dither is for averages in 8 bits")
     _on(device, grad_scale)
     if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
         raise ValueError("grad_scale must be one float32 element")
@@ -343,7 +346,7 @@ def adamw_step(params, grads, first, second, step, lr=1e-3, betas=(0.9, 0.999), 
     flat = array.array("q", itertools.chain.from_iterable(rows))
     st = _stream(device, stream, tensors + [grad_scale])
     options = binding.ADAMW_OPTIONS.pack(binding.ADAMW_OPTIONS.size, 8 if eight else 32, int(step), float(lr), float(betas[0]), float(betas[1]), float(eps),
-                                         float(weight_decay), grad_scale.data_ptr() if grad_scale is not None else 0, st, device.index)
+                                         float(weight_decay), grad_scale.data_ptr() if grad_scale is not None else 0, st, device.index, 1 if dither else 0)
     _check(load_library().nomad_adamw_step(flat.buffer_info()[0], count, options), "nomad_adamw_step")
 
 

@@ -92,7 +92,7 @@ class Placer:
         drouter, drouter_bias = grouped_weight_gradient(dlogits, x, one)
         self.steps += 1
         adamw_step(self.parameters(), [drouter, drouter_bias, g["dw1"], g["db1"], g["dw2"], g["db2"]], [s[0] for s in self._states],
-                   [s[1] for s in self._states], self.steps, lr=lr, weight_decay=weight_decay)
+                   [s[1] for s in self._states], self.steps, lr=lr, weight_decay=weight_decay, dither=self.bits == 8)
         return (off * off).sum(1).mean()
 
     @classmethod

@@ -429,6 +429,76 @@ def test_adamw_steps_of_small_gradients(eps, bits, dtype):
     assert np.all(np.abs(host(p) - want) <= (16 * U32 + UNIT[dtype]) * np.abs(want))
 
 
+@pytest.mark.parametrize("dtype,g_dtype", [(F32, F32), (BF16, BF16), (F16, F32)])
+def test_adamw_dithered_codes(dtype, g_dtype):
+    """Every code lies between the two borders that its element's draw gives, to the rounding of the average and of the borders."""
+    note(f"adamw dithered {dtype} {g_dtype}")
+    rng = np.random.default_rng(24)
+    params, grads = sizes_and_views(dtype, g_dtype, rng)
+    states = [nomad.adamw_state(p, 8) for p in params]
+    for step in (1, 2, 2 ** 33 + 5):
+        before = [(host(p), mo.decode_first(*(t.cpu().numpy() for t in m)), mo.decode_second(*(t.cpu().numpy() for t in v))) for p, (m, v) in zip(params, states)]
+        nomad.adamw_step(params, grads, [s[0] for s in states], [s[1] for s in states], step, lr=0.01, betas=(0.9, 0.99), eps=1e-6, weight_decay=0.1, dither=True)
+        for i, (p, g, (m, v)) in enumerate(zip(params, grads, states)):
+            wp, wm, wv = mo.adamw(before[i][0], host(g), before[i][1], before[i][2], step, 0.01, 0.9, 0.99, 1e-6, 0.1)
+            assert np.all(np.abs(host(p) - wp) <= UNIT[dtype] * np.abs(wp) + 2.0 ** -25 * (dtype == F16) + 32 * U32 * (np.abs(before[i][0]) + 0.2))
+            if not wm.size:
+                continue
+            for want, codes, most, power, second in ((wm, m, 127, 2, False), (wv, v, 255, 4, True)):
+                c, s = np.abs(codes.codes.cpu().numpy().astype(np.float64)), codes.scales.cpu().numpy().astype(np.float64)
+                top = np.array([np.abs(want[b:b + 256]).max() for b in range(0, want.size, 256)])
+                assert np.all(np.abs(s - top) <= 8 * U32 * top)
+                t, u = np.abs(want) * (most ** power / np.repeat(s, 256)[:want.size]), mo.draws(want.size, step, second)
+
+                def border(low):
+                    return low ** power + u * ((low + 1.0) ** power - low ** power)
+                slack = 64 * U32 * t
+                assert np.all((t - slack <= border(c)) | (c == most)) and c.max() <= most
+                assert np.all((t + slack >= border(c - 1.0)) | (c == 0) | (second & (c == 1)))
+                sign = np.sign(codes.codes.cpu().numpy().astype(np.float64))
+                assert np.all((sign == np.sign(want)) | (c == 0)) and np.all((c > 0) | (want == 0) | (not second))
+
+
+def test_adamw_dithered_averages_follow_changing_gradients():
+    """As in the oracle's test of the same name, by the kernel, with a third of the gradients ending altogether: their first averages reach
+    0 (at code 1 a draw keeps it nine times in ten), where nearest codes stop at 9."""
+    note("adamw dithered, 4,000 steps")
+    n, steps, beta2 = 6144, 4000, 0.999
+    kind = torch.arange(n, device="cuda") % 3
+    p = torch.zeros(n, device="cuda")
+    m, v = nomad.adamw_state(p, 8)
+    early, late = torch.ones(n, device="cuda"), torch.where(kind == 0, 1.0, torch.where(kind == 1, 0.03, 0.0)).float()
+    exact, variance = np.zeros(3), 0.0
+    for step in range(1, steps + 1):
+        nomad.adamw_step([p], [early if step <= 800 else late], [m], [v], step, lr=1e-3, betas=(0.9, beta2), weight_decay=0.0, dither=True)
+        exact = beta2 * exact + (1 - beta2) * (np.ones(3) if step <= 800 else np.array([1.0, 0.03 ** 2, 0.0]))
+        c = 255.0 * (exact[2] / exact[0]) ** 0.25
+        variance += (1 - beta2) * (4 / c + 6 / c ** 2)
+    shown, codes = host(nomad.adamw_state_values([v])[0]), m.codes.cpu().numpy()
+    kind = kind.cpu().numpy()
+    for which in (1, 2):
+        of = shown[kind == which]
+        note(f"  kind {which}: {of.mean() / exact[which] - 1:+.4f} of {6 * np.sqrt(variance / of.size):.4f}")
+        assert abs(of.mean() / exact[which] - 1) < 6 * np.sqrt(variance / of.size)
+    assert (codes[kind == 2] == 0).all() and (codes[kind == 0] == 127).all()
+
+
+def test_adamw_dither_is_the_same_every_time_and_not_for_32_bits():
+    note("adamw dither repeats")
+    rng = np.random.default_rng(25)
+    g = randn((5001,), F32, rng)
+    got = []
+    for step, stream in ((7, None), (7, torch.cuda.Stream().cuda_stream), (8, None)):
+        p = torch.zeros(5001, device="cuda")
+        m, v = nomad.adamw_state(p, 8)
+        nomad.adamw_step([torch.zeros(3, device="cuda"), p], [g[:3].clone(), g], [nomad.adamw_state(g[:3], 8)[0], m], [nomad.adamw_state(g[:3], 8)[1], v], step, dither=True, stream=stream)
+        torch.cuda.synchronize()
+        got.append(torch.cat([m.codes.int(), v.codes.int()]))
+    assert torch.equal(got[0], got[1]) and (got[0] != got[2]).float().mean() > 0.1
+    with pytest.raises(ValueError):
+        nomad.adamw_step([g], [g.clone()], [torch.zeros_like(g)], [torch.zeros_like(g)], 1, dither=True)
+
+
 # ---- streams and refusals
 
 

@@ -79,6 +79,41 @@ def test_adamw_first_step_is_the_sign():
     assert np.allclose(mo.adamw(np.array([1.0]), np.zeros(1), np.zeros(1), np.zeros(1), 1, 0.1, 0.9, 0.999, 1e-8, 0.5)[0], 0.95)
 
 
+def test_draws_are_philox_and_even():
+    from oracle import c_oracle
+    rng = np.random.default_rng(6)
+    for _ in range(20):
+        counter, key = rng.integers(0, 2 ** 32, size=4), rng.integers(0, 2 ** 32, size=2)
+        assert mo.philox(counter, key).tolist() == list(c_oracle.philox(counter.tolist(), key.tolist()))
+    u = mo.draws(100_003, 12345, True)
+    assert u.shape == (100_003,) and u.min() > 0 and u.max() < 1
+    assert abs(u.mean() - 0.5) < 6 / np.sqrt(12 * u.size) and (mo.draws(100_003, 12346, True) != u).mean() > 0.99
+    words = mo.philox([[2, 0, 0, 0]], (7, 0))[0]
+    assert mo.draws(24, 7, False)[16:20].tolist() == [(int(w) + 0.5) / 65536 for w in (words[0] & np.uint64(65535), words[0] >> np.uint64(16), words[1] & np.uint64(65535), words[1] >> np.uint64(16))]
+
+
+def test_dithered_averages_follow_changing_gradients():
+    """beta2 = 0.999, half of each block's gradients shrinking to 3 % after 1,000 of 5,000 steps.  A code's draw is right in expectation and the
+    average linear, so the decoded average is off by noise alone: a step's change of v by no more than 0.001 v is drawn from two codes whose
+    values are 4 / c + 6 / c^2 of v apart, a variance of no more than their product, and earlier noise decays no slower than v does."""
+    blocks, steps, beta2 = 4, 5000, 0.999
+    n = blocks * 256
+    small = np.arange(n) % 2 == 1
+    codes, scales, exact = np.zeros(n), np.zeros(blocks), np.zeros(n)
+    variance = 0.0
+    for step in range(1, steps + 1):
+        g = np.where(small & (step > 1000), 0.03, 1.0)
+        v = beta2 * mo.decode_second(codes, scales) + (1 - beta2) * g * g
+        exact = beta2 * exact + (1 - beta2) * g * g
+        codes, scales, _ = mo.encode_second(v, mo.draws(n, step, True))
+        c = 255.0 * (exact[1] / exact[0]) ** 0.25
+        variance += (1 - beta2) * (4 / c + 6 / c ** 2)
+    got = mo.decode_second(codes, scales)
+    assert abs(got[small].mean() / exact[1] - 1) < 6 * np.sqrt(variance / small.sum())
+    assert np.abs(got[~small] / exact[0] - 1).max() < 1e-6      # the largest of their blocks: code 255, no noise
+    assert np.sqrt(exact[1]) < 0.15 * np.sqrt(exact[0])         # (and they have become small)
+
+
 def test_codes_of_8_bits_are_the_nearest_at_any_scale():
     """Every code lies between its borders, and the value it stands for within half a step, for scales from one to the smallest."""
     rng = np.random.default_rng(5)
