@@ -17,7 +17,8 @@ bool by(const void* p, int64_t stride, int64_t size, int64_t bytes) { return ((u
 // in one than keep the counts well below the logits
 int64_t chunk_rows(int64_t n) { return std::max<int64_t>(256, (n + 1023) / 1024); }
 // One workgroup does it all where the logits are few (a row of 256: 4.4 us, the three kernels of the other form 12.4; 100 rows of 50: 6.4 against 40)
-bool is_small(int64_t n, int32_t n_experts) { return n * n_experts <= 32768 && n <= 1024; }
+// and its counters and slots fit the 64 KB of LDS that a launch has without asking
+bool is_small(int64_t n, int32_t n_experts, int32_t k) { return n * n_experts <= 32768 && n <= 1024 && n_experts + n * k <= 16384; }
 
 template <typename T, int LANES, int K>
 void launch_pick(const RouteArgs& p, bool vec, hipStream_t st) {
@@ -28,13 +29,13 @@ void launch_pick(const RouteArgs& p, bool vec, hipStream_t st) {
 }
 template <typename T, int LANES, int K>
 void launch_small(const RouteArgs& p, bool vec, hipStream_t st) {
-    const size_t lds = sizeof(int32_t) * (size_t)(p.n_experts + p.n * p.k);   // (n k <= 8 n, and n n_experts <= 32768: under 64 KB)
+    const size_t lds = sizeof(int32_t) * (size_t)(p.n_experts + p.n * p.k);
     if (vec) hipLaunchKernelGGL((k_route_small<T, LANES, K, true>), dim3(1), dim3(kSmallThreads), lds, st, p);
     else hipLaunchKernelGGL((k_route_small<T, LANES, K, false>), dim3(1), dim3(kSmallThreads), lds, st, p);
 }
 template <typename T, int K>
 void launch_route(const RouteArgs& p, bool vec, hipStream_t st) {
-    if (is_small(p.n, p.n_experts)) {
+    if (is_small(p.n, p.n_experts, p.k)) {
         // few rows: a wavefront each; more: four a wavefront, as long as a row is a few loads of 16 lanes
         if (p.n <= kSmallThreads / 64 || p.n_experts > 512) launch_small<T, 64, K>(p, vec, st);
         else launch_small<T, 16, K>(p, vec, st);
@@ -109,7 +110,7 @@ int use_device(int32_t device) {
 
 #pragma GCC visibility push(default)
 extern "C" int64_t nomad_route_workspace(int64_t n, int32_t n_experts, int32_t k) {
-    if (n <= 0 || n_experts < 1 || k < 1 || n > NOMAD_MAX_ROWS || n_experts > kMaxExperts || is_small(n, n_experts)) return 0;
+    if (n <= 0 || n_experts < 1 || k < 1 || n > NOMAD_MAX_ROWS || n_experts > kMaxExperts || is_small(n, n_experts, k)) return 0;
     return ((n + chunk_rows(n) - 1) / chunk_rows(n) + 1) * n_experts * (int64_t)sizeof(int32_t);
 }
 

@@ -95,6 +95,15 @@ def test_routing(n, experts, k, dtype, normalize):
     near(got, want, size, dtype, "dlogits")
 
 
+@pytest.mark.parametrize("n,experts,k,dtype", [(1, 16384, 8, F32), (2, 16384, 8, BF16), (1, 16377, 8, F16), (1, 16376, 8, F32), (2, 16370, 7, F32)])
+def test_routing_of_a_row_or_two_over_many_experts(n, experts, k, dtype):
+    """On either side of what one workgroup has LDS for."""
+    note(f"route n={n} E={experts} k={k} {dtype}")
+    rng = np.random.default_rng(n + experts + k)
+    for normalize in (True, False):
+        check_routing(torch.from_numpy(rng.normal(size=(n, experts)).astype(np.float32)).to("cuda", dtype), k, normalize)
+
+
 def test_routing_strides_extremes_and_rows_that_all_want_one_expert():
     note("route strides")
     rng = np.random.default_rng(1)
