@@ -62,15 +62,18 @@ def _rows(t, name, columns=None):
 
 
 def _stream(device, stream, used):
-    """The stream of a call.  What it uses of torch's memory is not handed out again before a stream other than the current one
-    has come by here."""
-    chosen = binding._call_stream(device.index, stream)
-    if stream is not None and chosen != torch._C._cuda_getCurrentRawStream(device.index):
-        other = torch.cuda.ExternalStream(int(chosen), device=device)
-        for t in used:
-            if t is not None and t.numel():
-                t.record_stream(other)
-    return int(chosen)
+    """The stream of a call.  One other than the current stream waits (the host does not) for what the current one has been given so
+    far: it may be making the inputs, or working on what a result's memory belonged to before; and what the call uses of
+    torch's memory is not handed out again before that stream has come by here."""
+    current = torch._C._cuda_getCurrentRawStream(device.index)   # the handle alone: a Stream object takes as long as a small copy
+    if stream is None or int(stream) == current:
+        return current
+    other = torch.cuda.ExternalStream(int(stream), device=device)
+    other.wait_stream(torch.cuda.current_stream(device))
+    for t in used:
+        if t is not None and t.numel():
+            t.record_stream(other)
+    return int(stream)
 
 
 def _check(rc, name):

@@ -541,6 +541,58 @@ def test_another_stream_and_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(held, fresh))
 
 
+def test_another_stream_waits_for_the_current_one_and_the_host_does_not():
+    note("another stream behind work of the current one")
+    rng = np.random.default_rng(31)
+    logits, big, product = randn((300, 40), F32, rng), torch.ones(8192, 8192, device="cuda"), torch.empty(8192, 8192, device="cuda")
+    side = torch.cuda.Stream()
+    want = nomad.route(logits, 2)
+    nomad.route(logits, 2, stream=side.cuda_stream)
+    torch.mm(big, big, out=product)
+    torch.cuda.synchronize()
+    fresh, done = torch.empty_like(logits), torch.cuda.Event()
+    for _ in range(40):                                                # some 7 ms each
+        torch.mm(big, big, out=product)
+    fresh.copy_(logits)                                                # the input comes after all that
+    done.record()
+    got = nomad.route(fresh, 2, stream=side.cuda_stream)
+    assert not done.query()                                            # the call is back, and the current stream still at work
+    side.synchronize()
+    assert done.query() and all(torch.equal(a, b) for a, b in zip(got, want))
+    with torch.cuda.stream(side):                                      # the other way round: the default stream is the other one
+        fresh = logits.clone()
+        got = nomad.route(fresh, 2, stream=0)
+        torch.cuda.current_stream().wait_stream(torch.cuda.default_stream())
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_graph_with_another_stream_in_it():
+    note("a graph with another stream")
+    rng = np.random.default_rng(32)
+    logits, x, w = randn((500, 40), F32, rng), randn((500, 64), BF16, rng), randn((40, 48, 64), BF16, rng, 0.1)
+    side = torch.cuda.Stream()
+
+    def whole(stream):
+        r = nomad.route(logits, 2)
+        y = nomad.grouped_product(x, w, r.offsets, order=r.order, per_row=2, stream=stream)
+        if stream is not None:
+            torch.cuda.current_stream().wait_stream(side)
+        return nomad.combine(y, r.slots, r.weights)
+    whole(side.cuda_stream)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = whole(side.cuda_stream)
+    for seed in (1, 2, 3):
+        logits.copy_(torch.randn(500, 40, generator=torch.Generator().manual_seed(seed)))
+        graph.replay()
+        torch.cuda.synchronize()
+        fresh = whole(None)
+        torch.cuda.synchronize()
+        assert torch.equal(held, fresh)
+
+
 def test_refusals():
     x, w = torch.zeros(10, 8, device="cuda"), torch.zeros(2, 4, 8, device="cuda")
     offsets = torch.tensor([0, 5, 10], dtype=torch.int32, device="cuda")
