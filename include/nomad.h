@@ -533,8 +533,9 @@ int nomad_pca_init(const float* X, int64_t n, int32_t d, float std0, float* thet
  * Conventions of these calls: all arrays are device memory of `device`; a call checks its arguments on the host (sizes,
  * types, strides, pointers, not what device arrays hold), enqueues its kernels on `stream` and returns without waiting; it
  * allocates nothing (work space is the caller's, of the size that the *_workspace function names) and copies nothing to or
- * from the host, so it can be recorded into a HIP graph.  Strides are in elements.  Results do not depend on timing: no atomics on
- * floating-point numbers.  Sums are held in float32.  Errors: NOMAD_E_INVALID_ARG, NOMAD_E_TOO_LARGE, NOMAD_E_HIP.
+ * from the host, so it can be recorded into a HIP graph; the thread's current device is left as it was.  Strides are in
+ * elements.  Results do not depend on timing: no atomics on floating-point numbers.  Sums are held in float32.  Errors:
+ * NOMAD_E_INVALID_ARG, NOMAD_E_TOO_LARGE, NOMAD_E_HIP.
  */
 #define NOMAD_F32 0
 #define NOMAD_BF16 1

@@ -20,7 +20,7 @@ HEADERS = [os.path.join(_PKG, "csrc", "nomad_kernels.h"), os.path.join(_PKG, "cs
            os.path.join(_PKG, "csrc", "pca_kernels.h"), os.path.join(_PKG, "csrc", "host_util.h"),
            os.path.join(_PKG, "csrc", "edge_plan.h"), os.path.join(_PKG, "csrc", "exchange_kernels.h"),
            os.path.join(_PKG, "csrc", "run_kernels.h"), os.path.join(_PKG, "csrc", "field_kernels.h"), os.path.join(_PKG, "csrc", "small_kernels.h"), os.path.join(_PKG, "csrc", "kmeans_plan.h"),
-           os.path.join(_PKG, "csrc", "grouped_kernels.h"), os.path.join(_PKG, "csrc", "grouped_launch.h"), os.path.join(_PKG, "csrc", "grouped_plan.h"), os.path.join(_PKG, "csrc", "route_kernels.h"), os.path.join(_PKG, "csrc", "adamw_kernels.h"),
+           os.path.join(_PKG, "csrc", "grouped_kernels.h"), os.path.join(_PKG, "csrc", "grouped_launch.h"), os.path.join(_PKG, "csrc", "grouped_plan.h"), os.path.join(_PKG, "csrc", "route_kernels.h"), os.path.join(_PKG, "csrc", "adamw_kernels.h"), os.path.join(_PKG, "csrc", "device_scope.h"),
            os.path.join(_ROOT, "include", "nomad.h")]
 
 

@@ -5,6 +5,7 @@
 #include <cstddef>
 
 #include "adamw_kernels.h"
+#include "device_scope.h"
 #include "host_util.h"
 #include "nomad.h"
 
@@ -64,9 +65,8 @@ extern "C" int nomad_adamw_step(const nomad_adamw_tensor* tensors, int32_t count
         if (t.n > kMostElements) return NOMAD_E_TOO_LARGE;
         if (t.n > 0 && (!t.p || !t.g || !t.m || !t.v || (o.bits == 8 && (!t.m_scale || !t.v_scale)))) return NOMAD_E_INVALID_ARG;
     }
-    int ndev = 0;
-    if (hipGetDeviceCount(&ndev) != hipSuccess || o.device >= ndev) return NOMAD_E_HIP;
-    KTRY(hipSetDevice(o.device));
+    const DeviceScope on(o.device);
+    if (!on.ok()) return NOMAD_E_HIP;
     hipStream_t st = (hipStream_t)o.stream;
     Batch b;
     b.s.keep = (float)(1.0 - o.lr * o.weight_decay);
@@ -111,9 +111,8 @@ extern "C" int nomad_adamw_state_values(const void* const* codes, const float* c
         if (n[i] < 0 || (n[i] > 0 && (!codes[i] || !scales[i] || !out[i]))) return NOMAD_E_INVALID_ARG;
         if (n[i] > kMostElements) return NOMAD_E_TOO_LARGE;
     }
-    int ndev = 0;
-    if (hipGetDeviceCount(&ndev) != hipSuccess || device >= ndev) return NOMAD_E_HIP;
-    KTRY(hipSetDevice(device));
+    const DeviceScope on(device);
+    if (!on.ok()) return NOMAD_E_HIP;
     hipStream_t st = (hipStream_t)stream;
     ValuesBatch b;
     b.count = 0;

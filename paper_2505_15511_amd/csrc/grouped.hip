@@ -3,6 +3,7 @@
 
 #include <atomic>
 
+#include "device_scope.h"
 #include "grouped_launch.h"
 #include "nomad.h"
 
@@ -43,9 +44,8 @@ extern "C" int nomad_grouped_product(const nomad_grouped_product_args* args) {
     if (a.rows > NOMAD_MAX_ROWS || a.x_rows > NOMAD_MAX_ROWS || a.n_groups > NOMAD_MAX_GROUPS || a.in > NOMAD_MAX_COLUMNS || a.out > NOMAD_MAX_COLUMNS) return NOMAD_E_TOO_LARGE;
     if (a.rows == 0) return NOMAD_OK;
     if (!a.offsets || !a.x || !a.w || !a.y || a.x_rows < 1 || (!a.order && a.x_rows < a.rows)) return NOMAD_E_INVALID_ARG;
-    int ndev = 0;
-    if (hipGetDeviceCount(&ndev) != hipSuccess || a.device >= ndev) return NOMAD_E_HIP;
-    KTRY(hipSetDevice(a.device));
+    const DeviceScope on(a.device);
+    if (!on.ok()) return NOMAD_E_HIP;
     hipStream_t st = (hipStream_t)a.stream;
     const int64_t size = size_of(a.dtype), out_size = size_of(a.out_dtype), chunk = 16 / size;
     ProductArgs p{};
@@ -95,9 +95,8 @@ extern "C" int nomad_grouped_weight_gradient(const nomad_grouped_gradient_args* 
     const int64_t need = nomad_grouped_gradient_workspace(a.rows, a.n_groups, a.in, a.out, a.dtype);
     if (need > 0 && (!a.workspace || a.workspace_bytes < need || (uintptr_t)a.workspace % 16)) return NOMAD_E_INVALID_ARG;
     if (!a.offsets || !a.dw || (a.rows > 0 && (!a.x || !a.dy || a.x_rows < 1 || (!a.order && a.x_rows < a.rows)))) return NOMAD_E_INVALID_ARG;
-    int ndev = 0;
-    if (hipGetDeviceCount(&ndev) != hipSuccess || a.device >= ndev) return NOMAD_E_HIP;
-    KTRY(hipSetDevice(a.device));
+    const DeviceScope on(a.device);
+    if (!on.ok()) return NOMAD_E_HIP;
     hipStream_t st = (hipStream_t)a.stream;
     const int64_t size = size_of(a.dtype), out_size = size_of(a.out_dtype), chunk = 16 / size;
     GradientArgs p{};

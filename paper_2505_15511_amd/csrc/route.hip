@@ -1,6 +1,7 @@
 // libnomad: the router of a learned map and the weighted sum over experts behind the C ABI of include/nomad.h (host side).
 #include <hip/hip_runtime.h>
 
+#include "device_scope.h"
 #include "host_util.h"
 #include "nomad.h"
 #include "route_kernels.h"
@@ -99,13 +100,6 @@ void launch_combine_vec(const CombineArgs& p, bool vec, hipStream_t st) {
     else launch_combine_lanes<T, 1>(p, st);
 }
 
-int use_device(int32_t device) {
-    int ndev = 0;
-    if (hipGetDeviceCount(&ndev) != hipSuccess || device >= ndev) return NOMAD_E_HIP;
-    KTRY(hipSetDevice(device));
-    return NOMAD_OK;
-}
-
 }  // namespace
 
 #pragma GCC visibility push(default)
@@ -123,7 +117,8 @@ extern "C" int nomad_route(const void* logits, int32_t dtype, int64_t n, int64_t
     if (!offsets || (n > 0 && (!logits || !experts || !weights || !order || !slots))) return NOMAD_E_INVALID_ARG;
     const int64_t need = nomad_route_workspace(n, n_experts, k);
     if (need > 0 && (!workspace || workspace_bytes < need)) return NOMAD_E_INVALID_ARG;
-    if (const int rc = use_device(device)) return rc;
+    const DeviceScope on(device);
+    if (!on.ok()) return NOMAD_E_HIP;
     hipStream_t st = (hipStream_t)stream;
     RouteArgs p{};
     p.logits = logits;
@@ -157,7 +152,8 @@ extern "C" int nomad_route_gradient(const void* logits, int32_t dtype, int64_t n
     if (n_experts > kMaxExperts || n > NOMAD_MAX_ROWS / k) return NOMAD_E_TOO_LARGE;
     if (n == 0) return NOMAD_OK;
     if ((!normalize && !logits) || !experts || !weights || !dweights || !dlogits) return NOMAD_E_INVALID_ARG;
-    if (const int rc = use_device(device)) return rc;
+    const DeviceScope on(device);
+    if (!on.ok()) return NOMAD_E_HIP;
     const RouteGradientArgs p{logits, n, stride, n_experts, k, normalize, experts, weights, dweights, dlogits};
     const int64_t size = size_of(dtype);
     const bool vec = (normalize || by(logits, stride, size, 16)) && by(dlogits, n_experts, size, 16);
@@ -175,7 +171,8 @@ extern "C" int nomad_combine(const void* values, int32_t dtype, int64_t n_values
     if (n > NOMAD_MAX_ROWS / k || n_values > NOMAD_MAX_ROWS || d > NOMAD_MAX_COLUMNS) return NOMAD_E_TOO_LARGE;
     if (n == 0) return NOMAD_OK;
     if ((n_values > 0 && !values) || !slots || !y) return NOMAD_E_INVALID_ARG;
-    if (const int rc = use_device(device)) return rc;
+    const DeviceScope on(device);
+    if (!on.ok()) return NOMAD_E_HIP;
     CombineArgs p{};
     p.values = values;
     p.values_stride = values_stride;
@@ -204,7 +201,8 @@ extern "C" int nomad_combine_gradient(const void* dy, int32_t dtype, int64_t dy_
     if (order && n_values != n * k) return NOMAD_E_INVALID_ARG;
     if (n == 0) return NOMAD_OK;
     if (!dy || !slots || (dweights && n_values > 0 && !values) || (!dvalues && !dweights)) return NOMAD_E_INVALID_ARG;
-    if (const int rc = use_device(device)) return rc;
+    const DeviceScope on(device);
+    if (!on.ok()) return NOMAD_E_HIP;
     CombineArgs p{};
     p.values = values;
     p.values_stride = values_stride;
