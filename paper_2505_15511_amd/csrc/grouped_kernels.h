@@ -56,30 +56,72 @@ template <> struct Elem<float> {
 
 template <int V> struct Constant { static constexpr int value = V; };
 
-__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }   // (the hardware's reciprocal: one unit in the last place)
+// FULL: for results in float32, good to a few units of their last place wherever z lies; the others to 2^-16 of themselves, of which a rounding to
+// 16 bits shows nothing.
+//
+// e^x for x in [-104, 88], the nearer end beyond it (and for a NaN): the hardware's power of two is good to a unit, but its argument x log2(e)
+// loses x 2^-24 to rounding, which FULL puts back
+template <bool FULL>
+__device__ __forceinline__ float exponential(float x) {
+    if (!FULL) return __expf(x);
+    x = __builtin_amdgcn_fmed3f(x, -104.f, 88.f);
+    const float power = x * 1.44269504f, rest = fmaf(x, 1.92596303e-8f, fmaf(x, 1.44269504f, -power)), e = __builtin_amdgcn_exp2f(power);
+    return fmaf(e, rest * 0.69314718f, e);
+}
+template <bool FULL>
+__device__ __forceinline__ float bell(float z) {   // e^(-z^2 / 2)
+    const float square = z * z, e = exponential<FULL>(-0.5f * square);
+    return FULL ? fmaf(e, -0.5f * fmaf(z, z, -square), e) : e;   // (with what the square's rounding lost)
+}
+template <bool FULL>   // (the hardware's reciprocal: one unit in the last place)
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + exponential<FULL>(-z)); }
 
-// 1 + erf(z / sqrt 2): Abramowitz and Stegun, formula 7.1.26, whose error of 1.5e-7 is that of the sum's rounding
-__device__ __forceinline__ float one_plus_erf(float z) {
-    const float x = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * x);
-    const float tail = ((((1.061405429f * t - 1.453152027f) * t + 1.421413741f) * t - 0.284496736f) * t + 0.254829592f) * t * __expf(-x * x);
+// 1 + erf(z / sqrt 2) = erfc(-z / sqrt 2), which below zero is small and keeps its digits this way: erfc(x) = e^(-x^2) t P(t) for x > 0 with
+// t = 1 / (1 + 0.4 x), where e^(x^2) erfc(x) / t is smooth from 1 (t = 1) to 0.4 / sqrt(pi) (t -> 0); P fitted to it by least squares of the relative
+// error with weights that level its peaks: 1.3e-7 (eighth degree), 4.8e-6 (sixth).  `e`: bell(z)
+template <bool FULL>
+__device__ __forceinline__ float one_plus_erf(float z, float e) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.4f * 0.70710678118654752f, 1.f));
+    float tail;
+    if (FULL) {
+        tail = fmaf(0.050258245f, t, -0.18288736f);
+        tail = fmaf(tail, t, 0.16906485f);
+        tail = fmaf(tail, t, -0.0055921078f);
+        tail = fmaf(tail, t, 0.14142513f);
+        tail = fmaf(tail, t, 0.16854335f);
+        tail = fmaf(tail, t, 0.20784256f);
+        tail = fmaf(tail, t, 0.22566961f);
+        tail = fmaf(tail, t, 0.22567587f);
+    } else {
+        tail = fmaf(-0.095308885f, t, 0.18682611f);
+        tail = fmaf(tail, t, 0.068062447f);
+        tail = fmaf(tail, t, 0.18213749f);
+        tail = fmaf(tail, t, 0.20694368f);
+        tail = fmaf(tail, t, 0.22565743f);
+        tail = fmaf(tail, t, 0.22567692f);
+    }
+    tail = tail * t * e;
     return z < 0.f ? tail : 2.f - tail;
 }
 
-template <int ACT>
+template <int ACT, bool FULL>
 __device__ __forceinline__ float activate(float z) {
     if (ACT == kRelu) return z < 0.f ? 0.f : z;                       // (a NaN stays one)
-    if (ACT == kSilu) return z * sigmoid(z);
-    if (ACT == kGelu) return 0.5f * z * one_plus_erf(z);
+    if (ACT == kSilu) return z * sigmoid<FULL>(z);
+    if (ACT == kGelu) return 0.5f * z * one_plus_erf<FULL>(z, bell<FULL>(z));
     return z;
 }
-template <int ACT>
+template <int ACT, bool FULL>
 __device__ __forceinline__ float activation_slope(float z) {
     if (ACT == kRelu) return z > 0.f ? 1.f : (z != z ? z : 0.f);
     if (ACT == kSilu) {
-        const float s = sigmoid(z);
+        const float s = sigmoid<FULL>(z);
         return s + z * s * (1.f - s);
     }
-    if (ACT == kGelu) return 0.5f * one_plus_erf(z) + z * 0.39894228040143268f * __expf(-0.5f * z * z);
+    if (ACT == kGelu) {
+        const float e = bell<FULL>(z);
+        return 0.5f * one_plus_erf<FULL>(z, e) + z * 0.39894228040143268f * e;
+    }
     return 1.f;
 }
 
@@ -635,7 +677,7 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_product(ProductArgs
 #pragma unroll
                                 for (int j = 0; j < N; ++j) z[j] = j < n ? from[j] : (T)0.f;
 #pragma unroll
-                            for (int j = 0; j < N; ++j) v[set][j] *= activation_slope<ACT>((float)z[j]);
+                            for (int j = 0; j < N; ++j) v[set][j] *= activation_slope<ACT, sizeof(O) == 4>((float)z[j]);
                         } else if (p.z_out) {
                             Rows16<Work, T>::put(patch, set, v[set], lane);
                         }
@@ -646,7 +688,7 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_grouped_product(ProductArgs
                     for (int set = 0; set < Work::kSets; ++set) {
                         if (!SLOPE && inside)
 #pragma unroll
-                            for (int j = 0; j < N; ++j) v[set][j] = activate<ACT>(v[set][j]);
+                            for (int j = 0; j < N; ++j) v[set][j] = activate<ACT, sizeof(O) == 4>(v[set][j]);
                         Rows16<Work, O>::put(patch, set, v[set], lane);
                     }
                     Rows16<Work, O>::template send<STORES>(patch, (O*)p.y + (done_first + r0) * p.y_stride + wave_column, p.y_stride, done_count - r0, p.out - wave_column, lane);
@@ -673,6 +715,7 @@ constexpr int kFewWaves = 8;
 template <typename T, typename O>
 __global__ void __launch_bounds__(64 * kFewWaves) k_grouped_few(ProductArgs p) {
     constexpr int epc = 16 / (int)sizeof(T), step = 4 * epc;   // k a step: a chunk for every lane group
+    constexpr bool full = sizeof(O) == 4;
     __shared__ f32x4 part[kFewWaves][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4, i = lane & 15;
     const int32_t across = (p.out + 15) / 16;
@@ -728,11 +771,11 @@ __global__ void __launch_bounds__(64 * kFewWaves) k_grouped_few(ProductArgs p) {
         float v = acc[j];
         if (inside && p.slope_at) {
             const float z = (float)((const T*)p.slope_at)[row * p.slope_stride + col];
-            v *= p.activation == kRelu ? activation_slope<kRelu>(z) : p.activation == kSilu ? activation_slope<kSilu>(z) : p.activation == kGelu ? activation_slope<kGelu>(z) : 1.f;
+            v *= p.activation == kRelu ? activation_slope<kRelu, full>(z) : p.activation == kSilu ? activation_slope<kSilu, full>(z) : p.activation == kGelu ? activation_slope<kGelu, full>(z) : 1.f;
         } else {
             if (inside && p.bias) v += (float)((const T*)p.bias)[(int64_t)it.group * p.bias_stride + col];
             if (p.z_out) ((T*)p.z_out)[row * p.z_stride + col] = (T)v;
-            if (inside) v = p.activation == kRelu ? activate<kRelu>(v) : p.activation == kSilu ? activate<kSilu>(v) : p.activation == kGelu ? activate<kGelu>(v) : v;
+            if (inside) v = p.activation == kRelu ? activate<kRelu, full>(v) : p.activation == kSilu ? activate<kSilu, full>(v) : p.activation == kGelu ? activate<kGelu, full>(v) : v;
         }
         ((O*)p.y)[row * p.y_stride + col] = (O)v;
     }

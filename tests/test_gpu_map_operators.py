@@ -3,6 +3,8 @@
 Tolerances are bounds: a float32 sum of K terms in any order is off by at most (K + 8) 2^-24 times the sum of their absolute
 values; an activation passes that on with a slope of at most 1.13 and adds its own rounding, a few units of 2^-24 times
 (1 + |z|) |z|; the result is rounded once to its type."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -201,6 +203,50 @@ def test_weight_gradient(groups, total, inner, out, dtype, kind, gathered):
         near(db, want_b, (longest + 8) * U32 * size_b, F32, "db")
     again, none = nomad.grouped_weight_gradient(dy, x, go, order=gd, per_row=per_row, bias=False, out_dtype=F32)
     assert none is None and torch.equal(again, nomad.grouped_weight_gradient(dy, x, go, order=gd, per_row=per_row, out_dtype=F32)[0])
+
+
+@pytest.mark.parametrize("rows", [6, 700])
+@pytest.mark.parametrize("name", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_activations_of_float32_results(rows, name, dtype):
+    """Relative to the result, by unit matrices, which leave z exact.  The exponential, a sum and a quotient take a few roundings; GELU's argument
+    is rounded before erfc, whose relative slope is z^2; a slope's two terms add up with their errors."""
+    note(f"float32 {name} rows={rows} {dtype}")
+    z = torch.cat([torch.linspace(-9, 9, rows * 64 - 64, dtype=torch.float64), torch.logspace(-30, 0, 32, dtype=torch.float64), -torch.logspace(-30, 0, 32, dtype=torch.float64)])
+    x = z.reshape(rows, 64).cuda().to(dtype)
+    z, eye, offsets = host(x), torch.eye(64, device="cuda", dtype=dtype)[None], torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    limit = 16 * U32 * (1.0 if name == "silu" else 1.0 + 0.25 * z * z)
+    if name == "silu":
+        s = 1.0 / (1.0 + np.exp(-z))
+        want, first, second = z * s, s, z * s * (1.0 - s)
+    else:
+        erfc, density = np.vectorize(math.erfc), np.exp(-0.5 * z * z) / math.sqrt(2.0 * math.pi)
+        first, second = 0.5 * erfc(-z / math.sqrt(2.0)), z * density
+        want = z * first
+    got = host(nomad.grouped_product(x, eye, offsets, activation=name, out_dtype=F32))
+    off = np.abs(got - want) / np.maximum(np.abs(want), 1e-37)
+    note(f"  {np.max(off / limit):.3f} of the bound")
+    assert np.all(off <= limit)
+    ones = torch.ones(1, 64, 1, device="cuda", dtype=dtype)
+    got = host(nomad.grouped_product(torch.ones(rows, 1, device="cuda", dtype=dtype), ones, offsets, activation=name, slope_at=x, out_dtype=F32))
+    off = np.abs(got - (first + second)) / (np.abs(first) + np.abs(second))
+    note(f"  slope: {np.max(off / limit):.3f} of the bound")
+    assert np.all(off <= limit)
+
+
+@pytest.mark.parametrize("rows", [6, 700])
+@pytest.mark.parametrize("name", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_activations_of_16_bit_results(rows, name, dtype):
+    """The result's rounding hides all but a 16th of it: 2^-16 of the result beside that, which the smallest numbers keep too."""
+    note(f"16 bits {name} rows={rows} {dtype}")
+    x = torch.linspace(-9, 9, rows * 64, dtype=torch.float64).reshape(rows, 64).cuda().to(dtype)
+    z, eye, offsets = host(x), torch.eye(64, device="cuda", dtype=dtype)[None], torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    want = z / (1.0 + np.exp(-z)) if name == "silu" else 0.5 * z * np.vectorize(math.erfc)(-z / math.sqrt(2.0))
+    off = np.abs(host(nomad.grouped_product(x, eye, offsets, activation=name)) - want)
+    limit = (UNIT[dtype] + 2.0 ** -16) * np.abs(want) + (2.0 ** -25 if dtype == F16 else 1e-37)
+    note(f"  {np.max(off / limit):.3f} of the bound")
+    assert np.all(off <= limit)
 
 
 def test_product_layouts():
