@@ -2,8 +2,8 @@
 
 `pipeline.project` ends with a table of points; a new vector has no row in it.  Here every cluster of the partition has an
 expert, a small network of two layers that has learned its region; a router, linear in the vector, chooses the experts that
-answer and weighs them, so that the map is continuous across borders; the step that fits them is AdamW.  Every operator is the
-library's; this module only calls one after the other.
+answer and weighs them, so that the map is continuous across borders; the step that fits them is AdamW.  Router, products, sums over
+experts and clusters, gradients and the step are the library's operators; scaling, the residual and the rows of a batch are torch's.
 
     theta, info = pipeline.project(X, n_clusters=256, return_info=True)
     placer = placement.Placer.fit(X, theta, info["labels"], info["n_clusters"])
@@ -99,20 +99,29 @@ class Placer:
     def fit(cls, X, theta, labels, n_clusters, hidden=128, k=2, epochs=10, batch=8192, lr=2e-3, bits=32, seed=0, return_losses=False):
         """A placer that has learned the projection theta [n, 2] of X [n, d] (float32, on the GPU) with the partition `labels`.
         The router starts from the clusters' centres (the nearest centre has the largest logit), the experts' last biases
-        from the clusters' places; the rate falls linearly to zero."""
+        from the clusters' places; the rate falls linearly to zero.  Two fits with the same arguments give the same map."""
         n, d = X.shape
-        placer = cls(d, n_clusters, hidden, min(k, n_clusters), 2, bits, seed, X.device)
         at = labels.long()
-        count = torch.bincount(at, minlength=n_clusters).clamp(min=1).float()[:, None]
+        low, high = (int(v) for v in at.aminmax()) if at.numel() else (0, 0)
+        if tuple(at.shape) != (n,) or low < 0 or high >= n_clusters:
+            raise ValueError(f"labels must be {n} whole numbers in 0..{n_clusters - 1}")
+        placer = cls(d, n_clusters, hidden, min(k, n_clusters), 2, bits, seed, X.device)
+        # sums over clusters: the gradient of weights of one column out, in an order that does not depend on timing
+        sizes, members = torch.bincount(at, minlength=n_clusters), torch.sort(at, stable=True).indices.int()
+        count, ends = sizes.clamp(min=1).float()[:, None], torch.nn.functional.pad(sizes.cumsum(0), (1, 0)).int()
+        ones = torch.ones(n, 1, device=X.device)
+
+        def sums(values):
+            return grouped_weight_gradient(ones, values.contiguous(), ends, order=members, bias=False)[0][:, 0]
         placer.shift = X.mean(0)
         placer.scale = 1.0 / (X - placer.shift).pow(2).mean().sqrt().clamp(min=1e-30)
         placer.spread = theta.pow(2).mean().sqrt().clamp(min=1e-30)
-        centres = torch.zeros(n_clusters, d, device=X.device).index_add_(0, at, placer._inputs(X)) / count
+        centres = sums(placer._inputs(X)) / count
         # -|x - c|^2 / 2 without what all experts have in common, in units of the squared distance to a row's own centre
         width = (placer._inputs(X) - centres[at]).pow(2).sum(1).mean().clamp(min=1e-30)
         placer.router.copy_(centres * (4.0 / width))
         placer.router_bias.copy_(centres.pow(2).sum(1) * (-2.0 / width))
-        placer.b2.copy_(torch.zeros(n_clusters, 2, device=X.device).index_add_(0, at, theta / placer.spread) / count)
+        placer.b2.copy_(sums(theta / placer.spread) / count)
         gen = torch.Generator(device=X.device).manual_seed(seed)
         per, losses = max(1, -(-n // batch)), []
         for epoch in range(epochs):

@@ -29,6 +29,56 @@ def test_fitted_map_places_new_vectors(bits):
     assert (one - places[3:4]).abs().max() < 1e-4 * placer.spread
 
 
+def _projected(n=5000):
+    X, _ = workloads.gmm_points(n + 1000, 50, 10, 25.0, 7, mix="equal", interleave=True)
+    X = X.cuda()
+    seen, new = X[:n].contiguous(), X[n:].contiguous()
+    theta, info = pipeline.project(seen, 10, k=15, n_epochs=100, return_info=True)
+    return seen, new, theta, info
+
+
+def test_two_fits_of_one_seed_are_the_same_map():
+    """Sums over clusters, like every operator's, do not depend on timing."""
+    print("placement twice", flush=True)
+    seen, new, theta, info = _projected()
+    for bits in (32, 8):
+        fits = [placement.Placer.fit(seen, theta, info["labels"], info["n_clusters"], hidden=32, epochs=2, batch=512, bits=bits) for _ in range(3)]
+        for other in fits[1:]:
+            assert all(torch.equal(a, b) for a, b in zip(fits[0].parameters(), other.parameters()))
+            assert torch.equal(fits[0](new), other(new))
+
+
+def test_the_start_is_made_of_the_clusters():
+    """Without a step: centres and places of the clusters, against sums in 64 bits (a float32 sum of n terms is off by n + 8 units of 2^-24
+    of their absolute sum, and what is made of it by a few more)."""
+    print("placement start", flush=True)
+    seen, new, theta, info = _projected()
+    labels, groups = info["labels"].long(), info["n_clusters"]
+    p = placement.Placer.fit(seen, theta, labels, groups, hidden=16, epochs=0)
+    unit = (seen.shape[0] + 32) * 2.0 ** -24
+    x, places = ((seen - p.shift) * p.scale).double(), (theta / p.spread).double()
+    centres = torch.stack([x[labels == e].mean(0) for e in range(groups)])
+    width = (x - centres[labels]).pow(2).sum(1).mean()
+    size = torch.stack([x[labels == e].abs().mean(0) for e in range(groups)])
+    assert ((p.router.double() - centres * (4.0 / width)).abs() <= 4 * unit * (4.0 / width) * (size + centres.abs())).all()
+    want = torch.stack([places[labels == e].mean(0) for e in range(groups)])
+    size = torch.stack([places[labels == e].abs().mean(0) for e in range(groups)])
+    assert ((p.b2.double() - want).abs() <= 4 * unit * size).all()
+    for bad in (labels + 1, labels[:-1]):
+        with pytest.raises(ValueError):
+            placement.Placer.fit(seen, theta, bad, groups, epochs=0)
+
+
+def test_fitting_betters_the_start():
+    """The start places a vector at its clusters' places; a fitted map places it nearer to its neighbour than that."""
+    print("placement against its start", flush=True)
+    seen, new, theta, info = _projected()
+    target = theta[torch.cdist(new, seen).argmin(1)]
+    off = [(placement.Placer.fit(seen, theta, info["labels"], info["n_clusters"], hidden=64, epochs=epochs, batch=1024)(new) - target).norm(dim=1).median().item() for epochs in (0, 30)]
+    print(f"  median distance: start {off[0]:.4f}, fitted {off[1]:.4f}", flush=True)
+    assert off[1] < off[0]
+
+
 def test_step_moves_against_the_gradient_of_the_loss():
     """The step's gradients against differences of the loss that it returns.  Every expert is chosen: the loss jumps where
     a shift of the router changes the choice."""
