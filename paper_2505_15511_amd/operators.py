@@ -3,7 +3,8 @@ include/nomad.h).
 
 Tensors live on one GPU; a call checks them, takes what it returns from torch's allocator, enqueues the library's kernels on the
 current stream (or `stream`) and returns without waiting.  Gradients are calls of their own: the framework has no
-tape.  Arguments that do not fit raise ValueError before anything is enqueued."""
+tape.  Tensors that do not fit each other raise ValueError, numbers that the library refuses NomadError, both before anything is
+enqueued."""
 from __future__ import annotations
 
 import array
@@ -59,6 +60,12 @@ def _rows(t, name, columns=None):
     if beside != 1 and columns > 1 and rows:
         raise ValueError(f"the columns of {name} must be contiguous (strides {t.stride()})")
     return rows, columns, apart if rows > 1 else columns
+
+
+def _matrix(t, name):
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix, got shape {tuple(t.shape)}")
+    return t.shape
 
 
 def _stream(device, stream, used):
@@ -120,7 +127,7 @@ def route_gradient(logits, routing, dweights, normalize=True, stream=None):
     _on(device, routing.experts, routing.weights, dweights)
     code = _dtype(logits, "logits")
     n, experts, stride = _rows(logits, "logits")
-    k = routing.experts.shape[1]
+    _, k = _matrix(routing.experts, "routing.experts")
     _whole(routing.experts, "routing.experts", torch.int32, (n, k))
     _whole(routing.weights, "routing.weights", torch.float32, (n, k))
     _whole(dweights, "dweights", torch.float32, (n, k))
@@ -139,8 +146,8 @@ def _grouping(x_rows, offsets, order, per_row, rows):
     if order is not None:
         if order.dtype != torch.int32 or order.dim() != 1 or not order.is_contiguous():
             raise ValueError("order must be a contiguous int32 tensor")
-        if int(per_row) < 1:
-            raise ValueError("per_row must be at least 1")
+        if not 1 <= int(per_row) < 2 ** 31:
+            raise ValueError("per_row must be at least 1, and 32 bits")
         places = order.shape[0]
         if places and not x_rows:
             raise ValueError("order asks for rows of an empty x")
@@ -156,7 +163,7 @@ def grouped_product(x, w, offsets, bias=None, activation=None, order=None, per_r
     device = x.device
     _on(device, w, offsets, bias, order, slope_at)
     code = _dtype(x, "x")
-    if activation not in ACTIVATIONS:
+    if not isinstance(activation, (str, type(None))) or activation not in ACTIVATIONS:
         raise ValueError(f"activation must be one of {sorted(k for k in ACTIVATIONS if k)}")
     x_rows, columns, x_stride = _rows(x, "x")
     shape = w.shape
@@ -180,7 +187,7 @@ def grouped_product(x, w, offsets, bias=None, activation=None, order=None, per_r
     if slope_at is not None:
         if bias is not None or keep:
             raise ValueError("slope_at goes without bias and keep")
-        if slope_at.dtype != x.dtype or slope_at.shape[0] != places:
+        if slope_at.dtype != x.dtype or _matrix(slope_at, "slope_at")[0] != places:
             raise ValueError(f"slope_at must be [{places}, {out}] of {x.dtype}")
         _, _, z_stride = _rows(slope_at, "slope_at", out)
     out_dtype = x.dtype if out_dtype is None else out_dtype
@@ -190,7 +197,7 @@ def grouped_product(x, w, offsets, bias=None, activation=None, order=None, per_r
     z = torch.empty(places, out, dtype=x.dtype, device=device) if keep else None
     st = _stream(device, stream, (x, w, offsets, bias, order, slope_at, y, z))
     a = binding.GROUPED_PRODUCT_ARGS.pack(
-        binding.GROUPED_PRODUCT_ARGS.size, code, _DTYPES[out_dtype], ACTIVATIONS[activation], groups, int(per_row), inner, out, places, x_rows,
+        binding.GROUPED_PRODUCT_ARGS.size, code, _DTYPES[out_dtype], ACTIVATIONS[activation], groups, int(per_row) if order is not None else 1, inner, out, places, x_rows,
         offsets.data_ptr(), order.data_ptr() if order is not None else 0, x.data_ptr(), x_stride, w.data_ptr(), sg if groups > 1 else 0, so, si,
         bias.data_ptr() if bias is not None else 0, bias.stride(0) if bias is not None and groups > 1 else 0,
         slope_at.data_ptr() if slope_at is not None else 0, z_stride, y.data_ptr(), out, z.data_ptr() if keep else 0, out, st, device.index)
@@ -222,7 +229,7 @@ def grouped_weight_gradient(dy, x, offsets, order=None, per_row=1, bias=True, ou
     work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
     st = _stream(device, stream, (x, dy, offsets, order, dw, db, work))
     a = binding.GROUPED_GRADIENT_ARGS.pack(
-        binding.GROUPED_GRADIENT_ARGS.size, code, _DTYPES[out_dtype], groups, int(per_row), inner, out, rows, x_rows, offsets.data_ptr(),
+        binding.GROUPED_GRADIENT_ARGS.size, code, _DTYPES[out_dtype], groups, int(per_row) if order is not None else 1, inner, out, rows, x_rows, offsets.data_ptr(),
         order.data_ptr() if order is not None else 0, dy.data_ptr(), dy_stride, x.data_ptr(), x_stride, dw.data_ptr(), db.data_ptr() if bias else 0,
         work.data_ptr() if need else 0, need, st, device.index)
     _check(lib.nomad_grouped_weight_gradient(a), "nomad_grouped_weight_gradient")
@@ -235,7 +242,7 @@ def combine(values, slots, weights=None, stream=None):
     _on(device, slots, weights)
     code = _dtype(values, "values")
     n_values, d, stride = _rows(values, "values")
-    n, k = slots.shape
+    n, k = _matrix(slots, "slots")
     _whole(slots, "slots", torch.int32, (n, k))
     if weights is not None:
         _whole(weights, "weights", torch.float32, (n, k))
@@ -253,7 +260,7 @@ def combine_gradient(dy, values, slots, weights=None, order=None, need_dvalues=T
     _on(device, dy, slots, weights, order)
     code = _dtype(values, "values")
     n_values, d, stride = _rows(values, "values")
-    n, k = slots.shape
+    n, k = _matrix(slots, "slots")
     _whole(slots, "slots", torch.int32, (n, k))
     if weights is not None:
         _whole(weights, "weights", torch.float32, (n, k))
@@ -261,7 +268,7 @@ def combine_gradient(dy, values, slots, weights=None, order=None, need_dvalues=T
         _whole(order, "order", torch.int32, (n * k,))
         if n_values != n * k:
             raise ValueError(f"order says {n * k} places, values has {n_values}")
-    if dy.dtype != values.dtype or dy.shape[0] != n:
+    if dy.dtype != values.dtype or _matrix(dy, "dy")[0] != n:
         raise ValueError(f"dy must be [{n}, {d}] of {values.dtype}")
     _, _, dy_stride = _rows(dy, "dy", d)
     if not need_dvalues and not need_dweights:

@@ -667,3 +667,24 @@ def test_refusals():
         with pytest.raises(NomadError):
             f()
     nomad.adamw_step([], [], [], [], 1)
+
+
+def test_refusals_of_other_shapes():
+    """Tensors of another number of dimensions and the like are refused as the rest is, not by an IndexError on the way."""
+    note("refusals of shapes")
+    x, w = torch.zeros(10, 8, device="cuda"), torch.zeros(2, 4, 8, device="cuda")
+    offsets, order = torch.tensor([0, 5, 10], dtype=torch.int32, device="cuda"), torch.zeros(10, dtype=torch.int32, device="cuda")
+    r = nomad.route(torch.zeros(10, 4, device="cuda"), 2)
+    none, line = torch.zeros((), device="cuda"), torch.zeros(10, device="cuda")
+    bad = [lambda: nomad.route(line, 2), lambda: nomad.route(none, 1), lambda: nomad.route_gradient(x[:, :4], r._replace(experts=r.experts.view(-1)), torch.zeros(10, 2, device="cuda")),
+           lambda: nomad.route_gradient(x[:, :4], r._replace(experts=none.int()), torch.zeros(10, 2, device="cuda")), lambda: nomad.grouped_product(line, w, offsets),
+           lambda: nomad.grouped_product(x, w, offsets, slope_at=none), lambda: nomad.grouped_product(x, w, offsets, slope_at=line), lambda: nomad.grouped_product(x, w, none.int()),
+           lambda: nomad.grouped_product(x, w, offsets, activation=["silu"]), lambda: nomad.grouped_product(x, w, offsets, activation=2),
+           lambda: nomad.grouped_product(x, w, offsets, order=order, per_row=2 ** 31), lambda: nomad.grouped_weight_gradient(x, x, offsets, order=order, per_row=2 ** 40),
+           lambda: nomad.grouped_weight_gradient(none, x, offsets), lambda: nomad.combine(x, r.slots.view(-1)), lambda: nomad.combine(x, none.int()),
+           lambda: nomad.combine_gradient(none, x, r.slots), lambda: nomad.combine_gradient(line, x, r.slots), lambda: nomad.combine_gradient(x, x, r.slots.view(-1))]
+    for i, f in enumerate(bad):
+        with pytest.raises(ValueError):
+            f()
+            note(f"refusal {i} did not happen")
+    assert nomad.grouped_product(x, w, offsets, per_row=2 ** 40).shape == (10, 4)     # (no order: not looked at)
