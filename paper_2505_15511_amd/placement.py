@@ -68,7 +68,9 @@ class Placer:
         return torch.arange(2, dtype=torch.int32, device=self.router.device) * n
 
     def _inputs(self, x):
-        return (x.float() - self.shift) * self.scale
+        if x.dim() != 2 or x.shape[1] != self.shift.shape[0]:
+            raise ValueError(f"vectors must be rows of {self.shift.shape[0]} columns, got shape {tuple(x.shape)}")
+        return ((x.float() - self.shift) * self.scale).contiguous()
 
     def _logits(self, x, one):
         return grouped_product(x, self.router[None], one, self.router_bias[None])
@@ -82,11 +84,13 @@ class Placer:
     def step(self, x, target, lr=1e-3, weight_decay=0.0):
         """One AdamW step on the mean squared distance between the places of x and target [m, 2]; returns that distance (a
         tensor on the GPU, in units of the plane's spread, before the step)."""
+        if not x.shape[0] or tuple(target.shape) != (x.shape[0], self.b2.shape[1]):
+            raise ValueError(f"a step takes vectors, and as many places of {self.b2.shape[1]} coordinates")
         x, one = self._inputs(x), self._one(x.shape[0])
         logits = self._logits(x, one)
         routing = route(logits, self.k)
         y, kept = experts(x, routing, self.w1, self.b1, self.w2, self.b2, keep=True)
-        off = y - target / self.spread
+        off = (y - target / self.spread).contiguous()
         g = experts_gradient(off * (2.0 / x.shape[0]), x, routing, self.w1, self.b1, self.w2, self.b2, kept, need_dx=False)
         dlogits = route_gradient(logits, routing, g["dweights"])
         drouter, drouter_bias = grouped_weight_gradient(dlogits, x, one)

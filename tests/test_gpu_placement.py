@@ -107,3 +107,25 @@ def test_step_moves_against_the_gradient_of_the_loss():
             flat[at] = old
             got, want = g.view(-1)[at].item(), (up - down) / (2 * h)
             assert abs(got - want) < 2e-2 * (abs(want) + g.abs().max().item()) + 1e-3, (name, at, got, want)
+
+
+def test_vectors_in_any_layout_and_number():
+    print("placement layouts", flush=True)
+    torch.manual_seed(6)
+    p, x = placement.Placer(20, 5, hidden=16, k=2, seed=1), torch.randn(64, 20, device="cuda")
+    want = p(x)
+    wide = torch.randn(64, 33, device="cuda")
+    wide[:, 5:25] = x
+    for same in (x.t().contiguous().t(), wide[:, 5:25], x.double()):
+        assert torch.equal(p(same), want)
+    assert p(x[:0]).shape == (0, 2)
+    target = torch.randn(64, 2, device="cuda")
+    pair = [placement.Placer(20, 5, hidden=16, k=2, seed=1) for _ in range(2)]
+    pair[0].step(x, target)
+    pair[1].step(x.t().contiguous().t(), target.t().contiguous().t())
+    assert all(torch.equal(a, b) for a, b in zip(pair[0].parameters(), pair[1].parameters()))
+    for bad in ((x[:0], target[:0]), (x, target[:63]), (x, target[:, 0]), (x[:, :19], target)):
+        with pytest.raises(ValueError):
+            p.step(*bad)
+    with pytest.raises(ValueError):
+        p(x[:, :19])
