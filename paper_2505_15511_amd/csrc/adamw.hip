@@ -43,9 +43,7 @@ void launch_kind(int kind, const Batch& b, bool eight, bool dither, hipStream_t 
 
 constexpr int64_t kMostBlocks = ((int64_t)1 << 24) - 1;     // of a launch: fewer than 2^32 lanes
 constexpr int64_t kMostElements = kMostBlocks * kChunk;     // of a tensor: 3.4e10
-int64_t chunks_of(int64_t n, int turns = 1) { return (n + (int64_t)kChunk * turns - 1) / ((int64_t)kChunk * turns); }
-// eight workgroups for each of 256 compute units
-constexpr int64_t kManyElements = (int64_t)256 * 8 * kChunk * kTurns;
+int64_t chunks_of(int64_t n) { return (n + kChunk - 1) / kChunk; }
 
 }  // namespace
 
@@ -80,9 +78,6 @@ extern "C" int nomad_adamw_step(const nomad_adamw_tensor* tensors, int32_t count
     b.s.step_low = (uint32_t)o.step;
     b.s.step_high = (uint32_t)((uint64_t)o.step >> 32);
     b.s.grad_scale = o.grad_scale;
-    int64_t total = 0;
-    for (int32_t i = 0; i < count; ++i) total += tensors[i].n;
-    b.turns = total >= kManyElements ? kTurns : 1;
     for (int kind = 0; kind < 7; ++kind) {
         b.count = 0;
         b.first[0] = 0;
@@ -93,9 +88,9 @@ extern "C" int nomad_adamw_step(const nomad_adamw_tensor* tensors, int32_t count
         for (int32_t i = 0; i < count; ++i) {
             const nomad_adamw_tensor& t = tensors[i];
             if (t.n == 0 || kind_of(t.p_dtype, t.g_dtype) != kind) continue;
-            if (b.count == kTensors || (b.count > 0 && b.first[b.count] + chunks_of(t.n, b.turns) > kMostBlocks)) flush();
+            if (b.count == kTensors || (b.count > 0 && b.first[b.count] + chunks_of(t.n) > kMostBlocks)) flush();
             b.t[b.count] = Tensor{t.p, t.g, t.m, t.v, t.m_scale, t.v_scale, t.n};
-            b.first[b.count + 1] = b.first[b.count] + (uint32_t)chunks_of(t.n, b.turns);
+            b.first[b.count + 1] = b.first[b.count] + (uint32_t)chunks_of(t.n);
             ++b.count;
         }
         flush();

@@ -33,9 +33,8 @@ namespace nomad_adamw {
 
 constexpr int kTensors = 64;              // a launch: their addresses are its arguments (under 4 KB)
 constexpr int kThreads = 256, kPer = 8;   // lanes a workgroup, elements a lane
-constexpr int kChunk = kThreads * kPer;   // elements a workgroup takes at a time
-constexpr int kTurns = 4;                 // and how often, where there are enough for every compute unit: 2,048 elements are little beside
-                                          // the search for their tensor and the first load's way (97 M elements in 8 bits: 202 us, 207 taken once)
+constexpr int kChunk = kThreads * kPer;   // elements a workgroup takes (four times as many: 97 M elements with 8-bit states and the averages read
+                                          // back 377 us, 370 so; with 32-bit states 522 and 509)
 constexpr int kBlock = 256;               // elements a scale
 constexpr int kLanes = kBlock / kPer;
 
@@ -56,7 +55,7 @@ struct Scalars {
 struct Batch {
     Tensor t[kTensors];
     uint32_t first[kTensors + 1];   // workgroup of each tensor
-    int32_t count, turns;
+    int32_t count;
     Scalars s;
 };
 
@@ -265,12 +264,9 @@ __global__ void __launch_bounds__(kThreads) k_adamw(Batch b) {
     const Tensor t = b.t[lo];
     const bool borders = aligned(t.p, sizeof(P) * 4 < 16 ? sizeof(P) * kPer : 16) && aligned(t.g, sizeof(G) * 4 < 16 ? sizeof(G) * kPer : 16) &&
                          aligned(t.m, EIGHT ? 8 : 16) && aligned(t.v, EIGHT ? 8 : 16);
-    int64_t first = (int64_t)(blockIdx.x - b.first[lo]) * b.turns * kChunk;
-    for (int turn = 0; turn < b.turns && first < t.n; ++turn, first += kChunk) {
-        const int64_t at = first + (int64_t)threadIdx.x * kPer;
-        if (borders && first + kChunk <= t.n) step8<P, G, EIGHT, DITHER, true>(t, b.s, at, kPer);
-        else step8<P, G, EIGHT, DITHER, false>(t, b.s, at, (int)(t.n - at > kPer ? kPer : t.n - at));   // (every lane stays: the block's largest is found by all)
-    }
+    const int64_t first = (int64_t)(blockIdx.x - b.first[lo]) * kChunk, at = first + (int64_t)threadIdx.x * kPer;
+    if (borders && first + kChunk <= t.n) step8<P, G, EIGHT, DITHER, true>(t, b.s, at, kPer);
+    else step8<P, G, EIGHT, DITHER, false>(t, b.s, at, (int)(t.n - at > kPer ? kPer : t.n - at));   // (every lane stays: the block's largest is found by all)
 }
 
 // 8-bit states as the values they stand for
