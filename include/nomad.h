@@ -620,6 +620,9 @@ int nomad_grouped_product(const nomad_grouped_product_args* args);
  *
  *   dy [rows, out], x [x_rows, in] of `dtype`;  dw [n_groups, out, in] of out_dtype (`dtype` or NOMAD_F32), contiguous;
  *   db NULL or [n_groups, out] fp32, contiguous
+ *
+ * The work space holds the sums of long groups' parts: two to four times [out, in + 1] fp32 a part, by the rows alone (the
+ * offsets are not known to the host).
  */
 typedef struct {
   uint32_t struct_size; /* = sizeof(nomad_grouped_gradient_args) */

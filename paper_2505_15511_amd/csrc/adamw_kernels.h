@@ -3,8 +3,9 @@
 //   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  p = (1 - lr wd) p - (lr / c1) m / (sqrt(v) / sqrt(c2) + eps)
 //
 // One pass over the elements, eight neighbouring ones a lane: bound by their bytes (28 an element in float32, 10 with 16-bit
-// parameters and 8-bit states), and with 8-bit states nearly as much by the arithmetic of decoding and encoding: 97 M elements in
-// bfloat16 with 8-bit states take 202 us, 4.9 TB/s of the 5.4 of a large copy.
+// parameters and 8-bit states), and with 8-bit states nearly as much by the arithmetic of decoding and encoding.  97 M elements, one step after
+// the other: in bfloat16 with 8-bit states 232 us, 4.2 TB/s of the 5.4 of a large copy; float32 287 (5.4 TB/s); 32-bit states 512 and, in
+// bfloat16, 408 (5.3 and 5.2).
 //
 // 8 bits: blocks of 256 elements (the 32 lanes of half a wavefront) have one float32 scale s, their largest magnitude.
 // m = s (c / 127) |c / 127| and v = s (c / 255)^4: codes are denser near zero, where most of a block's averages are (v spans
@@ -14,7 +15,7 @@
 // v's is 0 only where v is.  The averages round every operation once, without fused ones, and borders are compared in float32: the
 // codes are the same whatever computes them.  The step's root and quotient are rounded correctly; only where parameters of 16 bits have
 // states of 8 the hardware's root and reciprocal stand in (one unit in the last place each, 2^-15 and less of what the parameter's own
-// rounding is; 97 M elements 240 us, 303 with the others, which cost nothing where more bytes move), and not for denormal numbers,
+// rounding is; 97 M elements 232 us, 272 with the others, which cost nothing where more bytes move), and not for denormal numbers,
 // which that root takes for zero.
 //
 // Nearest codes hold an average where it is as long as a step changes it by less than half the way to the next code: v falls only
@@ -22,7 +23,7 @@
 // codes are right on average instead: the border between c and c + 1 lies at c^2 + u ((c + 1)^2 - c^2) (fourth powers for v), u drawn
 // evenly from (0, 1) for every element and step, so that the value that a code stands for is the average in expectation, and so are all
 // that follow from it.  u: 16 bits of Philox(counter = (element / 8, 0 for m or 1 for v), key = step); nothing is kept for it.  97 M elements
-// in bfloat16 302 us against 240 with nearest codes.
+// in bfloat16 252 us against 232 with nearest codes, in float32 318 against 287.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -43,11 +43,13 @@ void launch_route(const RouteArgs& p, bool vec, hipStream_t st) {
         return;
     }
     // 16 lanes a row as long as each reads it in a few loads: the row's best are found in four exchanges, not six, four rows at once
-    // (a million rows of 256: 224 us, 486 with 64 lanes)
+    // (a million rows of 256: 224 us, 486 with 64 lanes; whole calls on 262,144 rows of 64, 256, 512 and 1,024 in float32: 55, 78, 137 and 237 us
+    // with 16 lanes, 146, 154, 186 and 252 with 64; of 2,048, 434 and 463: the line could lie higher)
     if (p.n_experts <= 512) launch_pick<T, 16, K>(p, vec, st);
     else launch_pick<T, 64, K>(p, vec, st);
     hipLaunchKernelGGL(k_route_scan, dim3(blocks_of(p.n_experts, kScanColumns)), dim3(kScanThreads), 0, st, p);
-    // (four wavefronts' counters of 2,048 experts are 32 KB of LDS; two million slots: 28 us, 44 with one wavefront a chunk)
+    // (four wavefronts' counters of 2,048 experts are 32 KB of LDS; two million slots: 28 us, 44 with one wavefront a chunk; whole calls on 65,536
+    // rows of 1,024 and 2,048: 178 and 282 us, 183 and 287 with one)
     if (p.n_experts <= 2048) hipLaunchKernelGGL(k_route_place<4>, dim3((uint32_t)p.n_chunks), dim3(256), sizeof(int32_t) * 4 * (size_t)p.n_experts, st, p);
     else hipLaunchKernelGGL(k_route_place<1>, dim3((uint32_t)p.n_chunks), dim3(64), sizeof(int32_t) * (size_t)p.n_experts, st, p);
 }
@@ -61,7 +63,9 @@ void launch_route_k(const RouteArgs& p, bool vec, hipStream_t st) {
 
 template <typename T, int K>
 void launch_route_gradient(const RouteGradientArgs& p, bool vec, hipStream_t st) {
-    // (a million rows of 256: 187 us, 304 with 64 lanes a row: a wavefront then waits for one row's experts and weights, not for four)
+    // (a million rows of 256: 187 us, 304 with 64 lanes a row: a wavefront then waits for one row's experts and weights, not for four; 262,144 rows
+    // of 64, 256, 512 and 1,024 in float32: 19, 55, 107 and 202 us with 16 lanes, 37, 47, 101 and 201 with 64; with weights over all experts 44, 121,
+    // 285 and 670 with 16, 131, 162, 275 and 486 with 64)
     if (p.n_experts <= 512) {
         const dim3 grid = grid_of((p.n + 15) / 16);
         if (vec) hipLaunchKernelGGL((k_route_gradient<T, 16, K, true>), grid, dim3(256), 0, st, p);
