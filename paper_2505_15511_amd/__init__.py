@@ -10,16 +10,17 @@ from .binding import (Nomad, NomadError, NomadConfig, load_library, knn_in_clust
 # the learned map's operators take torch's tensors, so their module brings torch with it: it is imported with the first of them
 _OPERATORS = ("Routing", "State8", "adamw_state", "adamw_state_values", "adamw_step", "combine", "combine_gradient", "grouped_product",
               "grouped_weight_gradient", "route", "route_gradient")
-__all__ = [name for name in globals() if not name.startswith("_")] + list(_OPERATORS)
+__all__ = [name for name in globals() if not name.startswith("_")] + ["operators", *_OPERATORS]
 
 
 def __getattr__(name):
-    if name not in _OPERATORS:
+    if name not in __all__:
         raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
-    from . import operators
+    import importlib
+    operators = importlib.import_module(".operators", __name__)
     globals().update((each, getattr(operators, each)) for each in _OPERATORS)
     return globals()[name]
 
 
 def __dir__():
-    return sorted(set(globals()) | set(_OPERATORS))
+    return sorted(set(globals()) | set(__all__))

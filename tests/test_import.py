@@ -22,6 +22,12 @@ def test_the_package_comes_without_torch():
     assert run.returncode == 0, run.stderr
 
 
+def test_their_module_comes_when_asked_for():
+    run = _run("import paper_2505_15511_amd as nomad\nassert 'operators' in dir(nomad) and nomad.operators.route is nomad.route\n"
+               "import paper_2505_15511_amd.operators as again\nassert again is nomad.operators")
+    assert run.returncode == 0, run.stderr
+
+
 def test_operators_come_when_asked_for():
     run = _run(f"import paper_2505_15511_amd as nomad\nnames = {OPERATORS!r}\n"
                "from paper_2505_15511_amd import operators, route\n"
