@@ -524,7 +524,7 @@ int nomad_pca_init(const float* X, int64_t n, int32_t d, float std0, float* thet
                    void* stream);
 
 /*
- * ---- operators of a learned map: router, products grouped by expert, weighted sum, AdamW ----
+ * ---- operators of a learned map: routers, products grouped by expert and dense ones, weighted sum, AdamW, gradients' norm ----
  *
  * A map that has been fitted is a table of points; these are the operators of a function that places new vectors on it:
  * every region of the partition has an expert, a router chooses a row's experts, their products run over ragged groups of
@@ -707,6 +707,129 @@ int nomad_adamw_step(const nomad_adamw_tensor* tensors, int32_t count, const nom
  * each, into out[t]; the arrays of addresses are host memory. */
 int nomad_adamw_state_values(const void* const* codes, const float* const* scales, float* const* out, const int64_t* n, int32_t count, int32_t second,
                              int32_t device, void* stream);
+
+/*
+ * Routing by scores: as nomad_route, whose experts, weights, offsets, order, slots and workspace it takes, with
+ *   s_e = 1 / (1 + e^-l_e) (NOMAD_SCORE_SIGMOID) or e^l_e over the sum of e^l of all experts (NOMAD_SCORE_SOFTMAX),  c_e = s_e + bias[e].
+ *
+ *   bias        NULL, or [n_experts] fp32: it has a say in what is chosen, not in the weights
+ *   groups      the experts are cut into so many runs of n_experts / groups neighbours (which must be a whole number); a run's score is its largest c
+ *               (group_best = 1) or the sum of its two largest (2; of one where it has one). Only experts of the top_groups runs of
+ *               largest score, ties to the lower, are chosen; k <= top_groups (n_experts / groups).  1 and 1: no groups
+ *   experts     the k largest c in descending order, ties to the lower expert; -1 where there is none: an expert whose logit is -inf or NaN, or whose
+ *               c is, is never chosen
+ *   weights     scale times s_j, over the sum of the chosen's s where normalize = 1 (also where all of them are too small for a float)
+ *
+ * c and the runs' scores are compared as 64 bits have them, so that experts do not depend on how a 32-bit exponential is rounded. Without a
+ * bias experts (and runs with group_best = 1) are compared by their logits.  A softmax with a logit of +inf has no scores: its experts are
+ * then chosen by logits, and the weights are NaN.
+ */
+#define NOMAD_SCORE_SOFTMAX 0
+#define NOMAD_SCORE_SIGMOID 1
+#define NOMAD_ROUTE_MAX_GROUPS 64
+typedef struct {
+  uint32_t struct_size; /* = sizeof(nomad_scoring) */
+  int32_t score, normalize;
+  int32_t groups, top_groups, group_best;
+  const float* bias;
+  float scale; /* finite, not 0 */
+} nomad_scoring;
+int nomad_route_scored(const void* logits, int32_t dtype, int64_t n, int64_t stride, int32_t n_experts, int32_t k, const nomad_scoring* scoring, int32_t* experts,
+                       float* weights, int32_t* offsets, int32_t* order, int32_t* slots, void* workspace, int64_t workspace_bytes, int32_t device, void* stream);
+
+/* dlogits [n, n_experts] of `dtype`, contiguous, from dweights [n, k]: the gradient through the weights (what is chosen has none, and so
+ * has the bias).  scoring as in the call that made experts and weights; its bias and groups are not looked at. */
+int nomad_route_scored_gradient(const void* logits, int32_t dtype, int64_t n, int64_t stride, int32_t n_experts, int32_t k, const nomad_scoring* scoring,
+                                const int32_t* experts, const float* weights, const float* dweights, void* dlogits, int32_t device, void* stream);
+
+/* out[e] = bias[e] + rate where expert e has fewer rows in `offsets` (of nomad_route or nomad_route_scored) than the experts' mean, - rate
+ * where it has more: the step that evens out what a biased choice sends to the experts.  out may be bias. */
+int nomad_balance_bias(const float* bias, const int32_t* offsets, int32_t n_experts, float rate, float* out, int32_t device, void* stream);
+
+/*
+ * y = act(x W^T + bias) + residual, or (x W^T) act'(slope_at): a layer that all rows share.
+ *
+ *   x          [rows, in] of `dtype`, columns contiguous; W [out, in] of `dtype`, one of its strides 1 (a transposed view gives the
+ *              gradient of the rows); bias NULL or [out] of `dtype`
+ *   residual   NULL, or [rows, out] of `dtype`, rows residual_stride apart (0: one row for all)
+ *   slope_at   NULL, or z [rows, out] of `dtype`: the step back through an activation (without bias, residual and z_out)
+ *   y          [rows, out] of out_dtype (`dtype` or NOMAD_F32);  z_out NULL, or [rows, out] of `dtype`: the products with the bias,
+ *              before the activation.  Neither overlaps an input
+ *
+ * 16-bit operands are multiplied exactly and added up in float32; activation and residual follow in float32, and one rounding.
+ * The work space holds the sums of parts of a product that has few results for many products.
+ */
+typedef struct {
+  uint32_t struct_size; /* = sizeof(nomad_dense_args) */
+  int32_t dtype, out_dtype, activation;
+  int32_t in, out;
+  int64_t rows;
+  const void* x;
+  int64_t x_stride;
+  const void* w;
+  int64_t w_out_stride, w_in_stride;
+  const void* bias;
+  const void* residual;
+  int64_t residual_stride;
+  const void* slope_at;
+  int64_t slope_stride;
+  void* y;
+  int64_t y_stride;
+  void* z_out;
+  int64_t z_stride;
+  void* workspace; /* 16-byte aligned */
+  int64_t workspace_bytes;
+  void* stream;
+  int32_t device;
+} nomad_dense_args;
+int64_t nomad_dense_workspace(int64_t rows, int32_t in, int32_t out, int32_t dtype);
+int nomad_dense_product(const nomad_dense_args* args);
+
+/*
+ * Its gradients from dy [rows, out] of `dtype`: with dz = dy act'(z) (z [rows, out] of `dtype`, what the product left in z_out; without an
+ * activation dz is dy and z is not looked at)
+ *   dx = dz W   [rows, in] of `dtype`;   dw = dz^T x   [out, in] of out_dtype (`dtype` or NOMAD_F32), contiguous;   db = sum of dz   [out] fp32
+ * NULL: not asked for (db comes with dw alone).  The residual's gradient is dy.  dz is kept in `dtype`, as the products multiply it.
+ */
+typedef struct {
+  uint32_t struct_size; /* = sizeof(nomad_dense_gradient_args) */
+  int32_t dtype, out_dtype, activation;
+  int32_t in, out;
+  int64_t rows;
+  const void* dy;
+  int64_t dy_stride;
+  const void* z;
+  int64_t z_stride;
+  const void* x;
+  int64_t x_stride;
+  const void* w;
+  int64_t w_out_stride, w_in_stride;
+  void* dx;
+  int64_t dx_stride;
+  void* dw;
+  float* db;
+  void* workspace; /* 16-byte aligned */
+  int64_t workspace_bytes;
+  void* stream;
+  int32_t device;
+} nomad_dense_gradient_args;
+int64_t nomad_dense_gradient_workspace(int64_t rows, int32_t in, int32_t out, int32_t dtype, int32_t activation);
+int nomad_dense_gradient(const nomad_dense_gradient_args* args);
+
+/*
+ * The norm of many tensors together, sqrt of the sum of all their squares times |*grad_scale| (device memory; NULL: 1), and in scale
+ * (NULL: not asked for) what a step's gradients have to be multiplied by for a norm of at most max_norm: *grad_scale, times max_norm / norm
+ * where the norm is larger (NaN where it is NaN, 0 where it is infinite).  nomad_adamw_step takes it as its grad_scale.  Squares are
+ * added up in float64, always in the same order.  norm, scale: one fp32 each.  Tensors are contiguous, of any of the three types.
+ */
+typedef struct {
+  const void* g;
+  int64_t n;
+  int32_t dtype;
+} nomad_gradient;
+int64_t nomad_gradient_norm_workspace(int32_t count);
+int nomad_gradient_norm(const nomad_gradient* tensors, int32_t count, double max_norm, const float* grad_scale, float* norm, float* scale, void* workspace,
+                        int64_t workspace_bytes, int32_t device, void* stream);
 
 /* Text of the last error of this context ("" if none), or, after a successful nomad_set_graph that had to take a
  * slower path, the reason (see nomad_scatter_path, nomad_edge_pass).  Valid until the next call on it. */

@@ -205,3 +205,108 @@ def encode_second(v, u=None):
     scales, t = _scaled(v, 255.0 ** 4)
     codes = _codes(t, 4, 255, u)
     return np.where(t > 0, np.maximum(codes, 1.0), 0.0), scales, t
+
+
+# ---- routing by scores, dense products, the norm
+
+
+def scores(logits, score):
+    """s and its logarithm, -inf where there is no score."""
+    x = np.asarray(logits, dtype=np.float64)
+    x = np.where(np.isnan(x), -math.inf, x)
+    with np.errstate(over="ignore", divide="ignore", invalid="ignore"):
+        if score == "sigmoid":
+            s = 1.0 / (1.0 + np.exp(-x))
+            log_s = np.where(x > -math.inf, np.minimum(x, 0.0) - np.log1p(np.exp(-np.abs(x))), -math.inf)
+        else:
+            top = x.max(1, keepdims=True)
+            e = np.exp(x - np.where(np.isfinite(top), top, 0.0))
+            total = e.sum(1, keepdims=True)
+            s = e / total
+            log_s = np.where(x > -math.inf, x - np.where(np.isfinite(top), top, 0.0) - np.log(total), -math.inf)
+    return x, s, log_s
+
+
+def route_scored(logits, k, score="sigmoid", bias=None, groups=1, top_groups=1, group_best=1, normalize=True, scale=1.0):
+    """(experts, weights, offsets, order, slots): Python loops over rows, groups and slots."""
+    x, s, log_s = scores(logits, score)
+    n, n_experts = x.shape
+    size = n_experts // groups
+    experts, weights = np.full((n, k), -1, np.int32), np.zeros((n, k))
+    for i in range(n):
+        broken = score == "softmax" and not x[i].max() < math.inf
+        by_logit = bias is None or broken
+        c = x[i].copy() if by_logit else np.where(x[i] > -math.inf, s[i] + bias.astype(np.float64), -math.inf)
+        c[np.isnan(c)] = -math.inf
+        sums = c if not by_logit or group_best == 1 or broken else np.where(x[i] > -math.inf, s[i], -math.inf)
+        ranking = []
+        for g in range(groups):
+            there = sorted((v for v in sums[g * size:(g + 1) * size] if v > -math.inf), reverse=True)[:group_best]
+            if there:
+                ranking.append((-sum(there), g))
+        opened = [g for _, g in sorted(ranking)[:top_groups]]
+        row = sorted((-c[e], e) for g in opened for e in range(g * size, (g + 1) * size) if c[e] > -math.inf)[:k]
+        if not row:
+            continue
+        chosen = [e for _, e in row]
+        if broken:
+            share = np.full(len(chosen), math.nan)
+        elif normalize:
+            top = max(log_s[i, e] for e in chosen)
+            share = np.exp(np.array([log_s[i, e] - top for e in chosen]))
+            share /= share.sum()
+        else:
+            share = np.exp(log_s[i, chosen])
+        experts[i, :len(chosen)] = chosen
+        weights[i, :len(chosen)] = scale * share
+    order, offsets = [], [0]
+    flat = experts.reshape(-1)
+    for e in range(n_experts):
+        order.extend(np.flatnonzero(flat == e).tolist())
+        offsets.append(len(order))
+    slots = np.full(n * k, -1, np.int32)
+    slots[order] = np.arange(len(order))
+    return experts, weights, np.array(offsets, np.int32), np.array(order + [-1] * (n * k - len(order)), np.int32), slots.reshape(n, k)
+
+
+def route_scored_gradient(logits, experts, weights, dweights, score="sigmoid", normalize=True, scale=1.0):
+    """By the logarithms of the scores: d w_j = w_j (d log s_j [- sum w_i / scale d log s_i])."""
+    x, s, _ = scores(logits, score)
+    out = np.zeros(x.shape)
+    for i in range(x.shape[0]):
+        there = [j for j in range(experts.shape[1]) if experts[i, j] >= 0]
+        inner = sum(weights[i, j] * dweights[i, j] for j in there) / scale if normalize else 0.0
+        total = 0.0
+        for j in there:
+            back = weights[i, j] * (dweights[i, j] - inner)   # of log s_j
+            out[i, experts[i, j]] += back / (1.0 + math.exp(min(x[i, experts[i, j]], 700.0))) if score == "sigmoid" else back
+            total += back
+        if score == "softmax" and there and not normalize:
+            out[i] -= s[i] * total
+    return out
+
+
+def balance_bias(bias, offsets, rate):
+    count = np.diff(np.asarray(offsets, dtype=np.int64))
+    return np.asarray(bias, dtype=np.float64) + rate * np.sign(count.sum() - len(count) * count)
+
+
+def dense(x, w, bias=None, activation=None, residual=None, slope_at=None):
+    """(y, z, sum of the absolute products)."""
+    z = x @ w.T + (0.0 if bias is None else bias)
+    size = np.abs(x) @ np.abs(w).T + (0.0 if bias is None else np.abs(bias))
+    if slope_at is not None:
+        return z * slope(slope_at, activation), z, size
+    return act(z, activation) + (0.0 if residual is None else residual), z, size
+
+
+def dense_gradient(dy, x, w, activation=None, z=None):
+    """(dx, dw, db, dz)."""
+    dz = dy * (slope(z, activation) if activation not in (None, "none") else 1.0)
+    return dz @ w, dz.T @ x, dz.sum(0), dz
+
+
+def gradient_norm(grads, max_norm=math.inf, grad_scale=1.0):
+    """(norm, scale)."""
+    norm = abs(grad_scale) * math.sqrt(sum(float((np.asarray(g, dtype=np.float64) ** 2).sum()) for g in grads))
+    return norm, grad_scale if norm <= max_norm else grad_scale * (max_norm / norm)

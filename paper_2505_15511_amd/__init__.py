@@ -8,8 +8,8 @@ from .binding import (Nomad, NomadError, NomadConfig, load_library, knn_in_clust
                       PATH_BINNED_POOLED, PATH_FIXED_ATOMICS, PATH_NAMES, EDGES_ROWS, EDGES_RECORDS, EDGES_POOLED, EDGES_EXCHANGED, EDGES_LDS_SUMS, POOL_PICKS16, POOL_DISTINCT, POOL_STRATIFIED)  # noqa: F401
 
 # the learned map's operators take torch's tensors, so their module brings torch with it: it is imported with the first of them
-_OPERATORS = ("Routing", "State8", "adamw_state", "adamw_state_values", "adamw_step", "combine", "combine_gradient", "grouped_product",
-              "grouped_weight_gradient", "route", "route_gradient")
+_OPERATORS = ("Routing", "State8", "adamw_state", "adamw_state_values", "adamw_step", "balance_bias", "combine", "combine_gradient", "dense_gradient",
+              "dense_product", "gradient_norm", "grouped_product", "grouped_weight_gradient", "route", "route_gradient", "route_scored", "route_scored_gradient")
 __all__ = [name for name in globals() if not name.startswith("_")] + ["operators", *_OPERATORS]
 
 

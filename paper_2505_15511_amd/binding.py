@@ -28,7 +28,9 @@ EXPORTS = ["nomad_create", "nomad_destroy", "nomad_set_graph", "nomad_set_embedd
            "nomad_copy_probe", "nomad_gather_probe", "nomad_scatter_probe", "nomad_knn_in_clusters", "nomad_kmeans_lloyd", "nomad_neighbourhood_preservation",
            "nomad_random_triplet_accuracy", "nomad_random_triplet_accuracy_noalloc", "nomad_pca_init", "nomad_kmeans_lsh_init",
            "nomad_route_workspace", "nomad_route", "nomad_route_gradient", "nomad_grouped_product", "nomad_grouped_gradient_workspace",
-           "nomad_grouped_weight_gradient", "nomad_combine", "nomad_combine_gradient", "nomad_adamw_step", "nomad_adamw_state_values"]
+           "nomad_grouped_weight_gradient", "nomad_combine", "nomad_combine_gradient", "nomad_adamw_step", "nomad_adamw_state_values",
+           "nomad_route_scored", "nomad_route_scored_gradient", "nomad_balance_bias", "nomad_dense_workspace", "nomad_dense_product", "nomad_dense_gradient_workspace",
+           "nomad_dense_gradient", "nomad_gradient_norm_workspace", "nomad_gradient_norm"]
 
 
 class NomadConfig(C.Structure):
@@ -53,6 +55,10 @@ GROUPED_PRODUCT_ARGS = struct.Struct("@I7i2q3Pq" "P3q" "PqPqPqPq" "Pi4x")
 GROUPED_GRADIENT_ARGS = struct.Struct("@I6i4x2q2P" "PqPq" "PP" "Pq" "Pi4x")
 ADAMW_TENSOR = struct.Struct("@6Pq2i")
 ADAMW_OPTIONS = struct.Struct("@Iiq5dPPi4xq")
+SCORING = struct.Struct("@I5iPf4x")
+DENSE_ARGS = struct.Struct("@I5iq" "PqPqqP" "PqPqPqPq" "PqPi4x")
+DENSE_GRADIENT_ARGS = struct.Struct("@I5iq" "PqPqPqPqq" "PqPP" "PqPi4x")
+GRADIENT = struct.Struct("@Pqi4x")
 
 
 class NomadError(RuntimeError):
@@ -122,6 +128,18 @@ def load_library():
     lib.nomad_combine_gradient.argtypes = [vp, i32, i64, vp, i64, i64, i32, vp, vp, vp, i64, i32, vp, vp, i32, vp]
     lib.nomad_adamw_step.argtypes = [vp, i32, vp]
     lib.nomad_adamw_state_values.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp]
+    lib.nomad_route_scored.argtypes = [vp, i32, i64, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, i64, i32, vp]
+    lib.nomad_route_scored_gradient.argtypes = [vp, i32, i64, i64, i32, i32, vp, vp, vp, vp, vp, i32, vp]
+    lib.nomad_balance_bias.argtypes = [vp, vp, i32, C.c_float, vp, i32, vp]
+    lib.nomad_dense_workspace.argtypes = [i64, i32, i32, i32]
+    lib.nomad_dense_workspace.restype = i64
+    lib.nomad_dense_product.argtypes = [vp]
+    lib.nomad_dense_gradient_workspace.argtypes = [i64, i32, i32, i32, i32]
+    lib.nomad_dense_gradient_workspace.restype = i64
+    lib.nomad_dense_gradient.argtypes = [vp]
+    lib.nomad_gradient_norm_workspace.argtypes = [i32]
+    lib.nomad_gradient_norm_workspace.restype = i64
+    lib.nomad_gradient_norm.argtypes = [vp, i32, C.c_double, vp, vp, vp, vp, i64, i32, vp]
     lib.nomad_last_error.argtypes = [vp]
     lib.nomad_last_error.restype = C.c_char_p
     _lib = lib

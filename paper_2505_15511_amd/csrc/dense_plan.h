@@ -1,0 +1,57 @@
+// How a dense product is cut: rules on sizes alone, plain C++.
+#pragma once
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "grouped_plan.h"
+
+namespace nomad_dense {
+
+using nomad_grouped::tiles_of;
+
+// Tiles of the result, its contiguous columns x its rows
+enum Tile { k256 = 0, k128, k64, k16, kFew };   // 256x256, 128x128, 64x128, 16x256; few rows: 16 columns x up to 64 rows
+
+struct Plan {
+    Tile tile;
+    int64_t parts;     // the sum over k is cut into
+    int64_t length;    // k of a part, a multiple of a stage's
+    int64_t units;     // tiles times parts
+};
+
+constexpr int64_t kFewRows = 64;
+
+// rows x columns of the result, k of the sum; small: two-byte elements; few: rows are read as k runs on either side; whole: 16-byte chunks
+// on either side and of the result
+inline Plan plan(int64_t rows, int64_t columns, int64_t k, bool small, bool few, bool whole, int64_t units) {
+    Plan p;
+    const int64_t stage = small ? 64 : 32;
+    int64_t a, b, at_once;
+    if (few && rows <= kFewRows) { p.tile = kFew; a = 16; b = kFewRows; at_once = 2; }
+    else if (columns <= 16) { p.tile = k16; a = 16; b = 256; at_once = 2; }
+    else if (columns <= 64 || tiles_of(columns, 64) * 64 * 9 < tiles_of(columns, 128) * 128 * 8) { p.tile = k64; a = 64; b = 128; at_once = 2; }
+    else if (small && whole && tiles_of(rows, 256) * tiles_of(columns, 256) >= units) { p.tile = k256; a = 256; b = 256; at_once = 1; }
+    else { p.tile = k128; a = 128; b = 128; at_once = 2; }
+    const int64_t tiles = tiles_of(columns, a) * tiles_of(rows, b), stages = tiles_of(k, stage);
+    // where tiles leave units without work, the sum is cut, to no less than four stages
+    p.parts = std::max<int64_t>(1, std::min(units * at_once / tiles, stages / 4));
+    const int64_t per = std::max<int64_t>(1, tiles_of(stages, p.parts));
+    p.length = per * stage;
+    p.parts = std::max<int64_t>(1, tiles_of(stages, per));
+    p.units = tiles * p.parts;
+    return p;
+}
+
+// Rows of a part of dz = dy act'(z), whose sums over rows meet afterwards: parts for all units, with at least 64 rows, and no more than 512 of them
+struct SlopePlan { int64_t parts, length; };
+inline SlopePlan plan_slope(int64_t rows, int64_t columns, int64_t units) {
+    const int64_t strips = tiles_of(columns, 2048);   // (as many columns as a workgroup takes side by side, or fewer)
+    const int64_t parts = std::max<int64_t>(1, std::min({rows / 64, (int64_t)512, std::max<int64_t>(1, 8 * units / strips)}));
+    SlopePlan p;
+    p.length = std::max<int64_t>(1, tiles_of(rows, parts));
+    p.parts = std::max<int64_t>(1, tiles_of(rows, p.length));
+    return p;
+}
+
+}  // namespace nomad_dense

@@ -2,24 +2,11 @@
 #include <hip/hip_runtime.h>
 
 #include "device_scope.h"
-#include "host_util.h"
-#include "nomad.h"
-#include "route_kernels.h"
+#include "route_launch.h"
 
 using namespace nomad_router;
 
 namespace {
-
-bool is_dtype(int32_t dtype) { return dtype == NOMAD_F32 || dtype == NOMAD_BF16 || dtype == NOMAD_F16; }
-int64_t size_of(int32_t dtype) { return dtype == NOMAD_F32 ? 4 : 2; }
-bool by(const void* p, int64_t stride, int64_t size, int64_t bytes) { return ((uintptr_t)p | (uintptr_t)(stride * size)) % (uintptr_t)bytes == 0; }
-
-// Rows a chunk of the counts: their scan walks the chunks of an expert, so there are about a thousand at most, and no fewer rows
-// in one than keep the counts well below the logits
-int64_t chunk_rows(int64_t n) { return std::max<int64_t>(256, (n + 1023) / 1024); }
-// One workgroup does it all where the logits are few (a row of 256: 4.4 us, the three kernels of the other form 12.4; 100 rows of 50: 6.4 against 40)
-// and its counters and slots fit the 64 KB of LDS that a launch has without asking
-bool is_small(int64_t n, int32_t n_experts, int32_t k) { return n * n_experts <= 32768 && n <= 1024 && n_experts + n * k <= 16384; }
 
 template <typename T, int LANES, int K>
 void launch_pick(const RouteArgs& p, bool vec, hipStream_t st) {
@@ -47,11 +34,7 @@ void launch_route(const RouteArgs& p, bool vec, hipStream_t st) {
     // with 16 lanes, 146, 154, 186 and 252 with 64; of 2,048, 434 and 463: the line could lie higher)
     if (p.n_experts <= 512) launch_pick<T, 16, K>(p, vec, st);
     else launch_pick<T, 64, K>(p, vec, st);
-    hipLaunchKernelGGL(k_route_scan, dim3(blocks_of(p.n_experts, kScanColumns)), dim3(kScanThreads), 0, st, p);
-    // (four wavefronts' counters of 2,048 experts are 32 KB of LDS; two million slots: 28 us, 44 with one wavefront a chunk; whole calls on 65,536
-    // rows of 1,024 and 2,048: 178 and 282 us, 183 and 287 with one)
-    if (p.n_experts <= 2048) hipLaunchKernelGGL(k_route_place<4>, dim3((uint32_t)p.n_chunks), dim3(256), sizeof(int32_t) * 4 * (size_t)p.n_experts, st, p);
-    else hipLaunchKernelGGL(k_route_place<1>, dim3((uint32_t)p.n_chunks), dim3(64), sizeof(int32_t) * (size_t)p.n_experts, st, p);
+    launch_places(p, st);
 }
 template <typename T>
 void launch_route_k(const RouteArgs& p, bool vec, hipStream_t st) {
@@ -126,20 +109,9 @@ extern "C" int nomad_route(const void* logits, int32_t dtype, int64_t n, int64_t
     hipStream_t st = (hipStream_t)stream;
     RouteArgs p{};
     p.logits = logits;
-    p.n = n;
     p.stride = stride;
-    p.n_experts = n_experts;
-    p.k = k;
     p.normalize = normalize;
-    p.experts = experts;
-    p.weights = weights;
-    p.offsets = offsets;
-    p.order = order;
-    p.slots = slots;
-    p.chunk = (int32_t)chunk_rows(n);
-    p.n_chunks = (int32_t)((n + p.chunk - 1) / p.chunk);
-    p.counts = (int32_t*)workspace;
-    p.totals = (int32_t*)workspace + (int64_t)p.n_chunks * n_experts;
+    fill_places(p, n, n_experts, k, experts, weights, offsets, order, slots, workspace);
     const int64_t size = size_of(dtype);
     const bool vec = by(logits, stride, size, 16) && n_experts % (16 / size) == 0;
     if (dtype == NOMAD_F32) launch_route_k<float>(p, vec, st);

@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(kPickThreads) k_route_pick(RouteArgs p) {
 }
 
 // 16 experts a workgroup, the chunks cut into 64 runs
-__global__ void __launch_bounds__(kScanThreads) k_route_scan(RouteArgs p) {
+static __global__ void __launch_bounds__(kScanThreads) k_route_scan(RouteArgs p) {
     __shared__ int32_t part[kScanThreads / kScanColumns][kScanColumns];
     constexpr int runs = kScanThreads / kScanColumns;
     const int col = threadIdx.x % kScanColumns, run = threadIdx.x / kScanColumns;
@@ -272,11 +272,28 @@ __global__ void __launch_bounds__(64 * WAVES) k_route_place(RouteArgs p) {
 }
 
 constexpr int kSmallThreads = 1024;
+// The end of a call that one workgroup does: counts of the experts in `next` to places and offsets, by its first wavefront
+__device__ __forceinline__ void place_few(const RouteArgs& p, int32_t* next, const int32_t* slots, int tid) {
+    if (tid >= 64) return;
+    const int lane = tid;
+    int32_t before = 0;
+    for (int32_t e0 = 0; e0 < p.n_experts; e0 += 64) {
+        const int32_t e = e0 + lane, total = e < p.n_experts ? next[e] : 0;
+        const int32_t upto = before + lanes_inclusive(total, lane);
+        if (e < p.n_experts) { next[e] = upto - total; p.offsets[e] = upto - total; }
+        before = __shfl(upto, 63);
+    }
+    if (lane == 0) p.offsets[p.n_experts] = before;
+    for (int64_t s = before + lane; s < p.n * p.k; s += 64) p.order[s] = -1;
+    __builtin_amdgcn_wave_barrier();
+    place_slots(p, slots, 0, p.n * p.k, next, lane);
+}
+
 template <typename T, int LANES, int K, bool VEC>
 __global__ void __launch_bounds__(kSmallThreads) k_route_small(RouteArgs p) {
     extern __shared__ int32_t next[];   // [n_experts], behind it the experts of the slots [n k]
     int32_t* slots = next + p.n_experts;
-    const int tid = threadIdx.x, lane = tid & 63, sub = tid % LANES;
+    const int tid = threadIdx.x, sub = tid % LANES;
     for (int32_t e = tid; e < p.n_experts; e += kSmallThreads) next[e] = 0;
     __syncthreads();
     for (int64_t i = tid / LANES; i < p.n; i += kSmallThreads / LANES) {
@@ -293,18 +310,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_route_small(RouteArgs p) {
             }
     }
     __syncthreads();
-    if (tid >= 64) return;
-    int32_t before = 0;
-    for (int32_t e0 = 0; e0 < p.n_experts; e0 += 64) {
-        const int32_t e = e0 + lane, total = e < p.n_experts ? next[e] : 0;
-        const int32_t upto = before + lanes_inclusive(total, lane);
-        if (e < p.n_experts) { next[e] = upto - total; p.offsets[e] = upto - total; }
-        before = __shfl(upto, 63);
-    }
-    if (lane == 0) p.offsets[p.n_experts] = before;
-    for (int64_t s = before + lane; s < p.n * p.k; s += 64) p.order[s] = -1;
-    __builtin_amdgcn_wave_barrier();
-    place_slots(p, slots, 0, p.n * p.k, next, lane);
+    place_few(p, next, slots, tid);
 }
 
 struct RouteGradientArgs {

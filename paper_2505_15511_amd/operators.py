@@ -1,5 +1,5 @@
-"""The operators of a learned map: router, products grouped by expert, weighted sum, AdamW (the second half of
-include/nomad.h).
+"""The operators of a learned map: routers, products grouped by expert and dense ones, weighted sum, AdamW, the gradients' norm (the second
+half of include/nomad.h).
 
 Tensors live on one GPU; a call checks them, takes what it returns from torch's allocator, enqueues the library's kernels on the
 current stream (or `stream`) and returns without waiting.  Gradients are calls of their own: the framework has no
@@ -10,6 +10,7 @@ from __future__ import annotations
 import array
 import ctypes as C
 import itertools
+import math
 import operator
 from typing import NamedTuple
 
@@ -19,6 +20,8 @@ from . import binding
 from .binding import NomadError, load_library
 
 MAX_K, MAX_EXPERTS, BLOCK = 8, 16384, 256
+MAX_GROUPS = 64
+SCORES = {"softmax": 0, "sigmoid": 1}
 ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3}
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _get_dtype = operator.attrgetter("dtype")
@@ -138,6 +141,86 @@ def route_gradient(logits, routing, dweights, normalize=True, stream=None):
     return out
 
 
+def _scoring(score, normalize, groups, top_groups, group_best, bias, scale):
+    if not isinstance(score, str) or score not in SCORES:
+        raise ValueError(f"score must be one of {sorted(SCORES)}")
+    return binding.SCORING.pack(binding.SCORING.size, SCORES[score], 1 if normalize else 0, groups, top_groups, group_best, bias.data_ptr() if bias is not None else 0, scale)
+
+
+def _scale(scale):
+    scale = float(scale)
+    if not math.isfinite(scale) or not 1e-37 < abs(scale) < 1e37:
+        raise ValueError("scale must be a float32 number other than 0")
+    return scale
+
+
+def route_scored(logits, k, score="sigmoid", bias=None, groups=1, top_groups=1, group_best=1, normalize=True, scale=1.0, stream=None) -> Routing:
+    """nomad_route_scored: the k experts of every row [n, n_experts] with the largest score ("sigmoid" or "softmax" of the logits) plus
+    bias (None, or float32 [n_experts]: it has a say in the choice alone), in the top_groups of `groups` runs of neighbouring experts, by
+    their group_best (1 or 2) largest; weights are scale times the scores, renormalised or not.  Returns what `route` returns."""
+    device = logits.device
+    _on(device, bias)
+    code = _dtype(logits, "logits")
+    n, experts, stride = _rows(logits, "logits")
+    k, groups, top_groups, group_best = int(k), int(groups), int(top_groups), int(group_best)
+    if not 1 <= k <= min(MAX_K, experts) or experts > MAX_EXPERTS:
+        raise ValueError(f"k = {k} of {experts} experts: 1 <= k <= {MAX_K} and no more than there are (at most {MAX_EXPERTS})")
+    if not 1 <= groups <= MAX_GROUPS or experts % groups:
+        raise ValueError(f"{experts} experts are not cut into {groups} groups (at most {MAX_GROUPS})")
+    if not 1 <= top_groups <= groups or group_best not in (1, 2) or k > top_groups * (experts // groups):
+        raise ValueError(f"{top_groups} of {groups} groups by their {group_best} best: 1 <= top_groups <= groups, group_best 1 or 2, and room for k = {k}")
+    if bias is not None:
+        _whole(bias, "bias", torch.float32, (experts,))
+    scoring = _scoring(score, normalize, groups, top_groups, group_best, bias, _scale(scale))
+    lib = load_library()
+    need = lib.nomad_route_workspace(n, experts, k)
+    chosen, slots = torch.empty(n, k, dtype=torch.int32, device=device), torch.empty(n, k, dtype=torch.int32, device=device)
+    weights, order = torch.empty(n, k, dtype=torch.float32, device=device), torch.empty(n * k, dtype=torch.int32, device=device)
+    offsets = torch.empty(experts + 1, dtype=torch.int32, device=device)
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    st = _stream(device, stream, (logits, bias, chosen, weights, offsets, order, slots, work))
+    _check(lib.nomad_route_scored(logits.data_ptr(), code, n, stride, experts, k, scoring, chosen.data_ptr(), weights.data_ptr(), offsets.data_ptr(), order.data_ptr(),
+                                  slots.data_ptr(), work.data_ptr() if need else None, need, device.index, st or None), "nomad_route_scored")
+    return Routing(chosen, weights, offsets, order, slots)
+
+
+def route_scored_gradient(logits, routing, dweights, score="sigmoid", normalize=True, scale=1.0, stream=None):
+    """nomad_route_scored_gradient: the gradient of the logits from that of the weights; score, normalize and scale as in the call of
+    `route_scored`.  The bias has none (`balance_bias` is its step)."""
+    device = logits.device
+    _on(device, routing.experts, routing.weights, dweights)
+    code = _dtype(logits, "logits")
+    n, experts, stride = _rows(logits, "logits")
+    _, k = _matrix(routing.experts, "routing.experts")
+    _whole(routing.experts, "routing.experts", torch.int32, (n, k))
+    _whole(routing.weights, "routing.weights", torch.float32, (n, k))
+    _whole(dweights, "dweights", torch.float32, (n, k))
+    scoring = _scoring(score, normalize, 1, 1, 1, None, _scale(scale))
+    out = torch.empty(n, experts, dtype=logits.dtype, device=device)
+    st = _stream(device, stream, (logits, routing.experts, routing.weights, dweights, out))
+    _check(load_library().nomad_route_scored_gradient(logits.data_ptr(), code, n, stride, experts, k, scoring, routing.experts.data_ptr(), routing.weights.data_ptr(),
+                                                      dweights.data_ptr(), out.data_ptr(), device.index, st or None), "nomad_route_scored_gradient")
+    return out
+
+
+def balance_bias(bias, offsets, rate, stream=None):
+    """nomad_balance_bias: bias [n_experts], float32, with `rate` more for experts that have fewer rows than the mean (offsets of a
+    routing), and less for those that have more; a new tensor."""
+    device = bias.device
+    _on(device, offsets)
+    if bias.dim() != 1 or not 1 <= bias.shape[0] <= MAX_EXPERTS:
+        raise ValueError(f"bias must be a tensor of 1 to {MAX_EXPERTS} experts, got shape {tuple(bias.shape)}")
+    experts = bias.shape[0]
+    _whole(bias, "bias", torch.float32, (experts,))
+    _whole(offsets, "offsets", torch.int32, (experts + 1,))
+    if not math.isfinite(rate):
+        raise ValueError("rate must be a number")
+    out = torch.empty_like(bias)
+    st = _stream(device, stream, (bias, offsets, out))
+    _check(load_library().nomad_balance_bias(bias.data_ptr(), offsets.data_ptr(), experts, float(rate), out.data_ptr(), device.index, st or None), "nomad_balance_bias")
+    return out
+
+
 def _grouping(x_rows, offsets, order, per_row, rows):
     """Checks of what says which row of x stands at which place; the number of places."""
     if offsets.dtype != torch.int32 or offsets.dim() != 1 or not offsets.is_contiguous() or offsets.shape[0] < 2:
@@ -236,6 +319,99 @@ def grouped_weight_gradient(dy, x, offsets, order=None, per_row=1, bias=True, ou
     return dw, db
 
 
+def _weights(w, dtype, columns):
+    """(out, in, strides) of a weight matrix in either order."""
+    shape = w.shape
+    if len(shape) != 2 or w.dtype != dtype or (columns is not None and shape[1] != columns) or 0 in shape:
+        raise ValueError(f"w must be [out, {'in' if columns is None else columns}] of {dtype}, got {tuple(shape)} of {w.dtype}")
+    out, inner = shape
+    so, si = w.stride()
+    if inner == 1:
+        si = 1
+    if out == 1 and si != 1:
+        so = 1
+    if si != 1 and so != 1:
+        raise ValueError(f"one of the strides of w must be 1 (strides {w.stride()}): .contiguous() copies it")
+    return out, inner, so, si
+
+
+def _activation(activation):
+    if not isinstance(activation, (str, type(None))) or activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(k for k in ACTIVATIONS if k)}")
+    return ACTIVATIONS[activation]
+
+
+def dense_product(x, w, bias=None, activation=None, residual=None, keep=False, slope_at=None, out_dtype=None, stream=None):
+    """nomad_dense_product: y = act(x w^T + bias) + residual, x [n, in], w [out, in] in either order of its strides, bias [out],
+    residual [n, out]; keep=True returns (y, z) with z the products before the activation; slope_at=z multiplies by the activation's slope at z
+    instead (the way back)."""
+    device = x.device
+    _on(device, w, bias, residual, slope_at)
+    code, act = _dtype(x, "x"), _activation(activation)
+    n, columns, x_stride = _rows(x, "x")
+    out, inner, so, si = _weights(w, x.dtype, columns)
+    if bias is not None:
+        _whole(bias, "bias", x.dtype, (out,))
+    if slope_at is not None and (bias is not None or residual is not None or keep):
+        raise ValueError("slope_at goes without bias, residual and keep")
+    strides = [0, 0]
+    for i, (t, name) in enumerate(((residual, "residual"), (slope_at, "slope_at"))):
+        if t is not None:
+            if t.dtype != x.dtype or _matrix(t, name)[0] != n:
+                raise ValueError(f"{name} must be [{n}, {out}] of {x.dtype}")
+            strides[i] = _rows(t, name, out)[2]
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    if out_dtype not in (x.dtype, torch.float32):
+        raise ValueError("out_dtype must be x's type or float32")
+    lib = load_library()
+    y = torch.empty(n, out, dtype=out_dtype, device=device)
+    z = torch.empty(n, out, dtype=x.dtype, device=device) if keep else None
+    need = lib.nomad_dense_workspace(n, inner, out, code)
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    st = _stream(device, stream, (x, w, bias, residual, slope_at, y, z, work))
+    a = binding.DENSE_ARGS.pack(
+        binding.DENSE_ARGS.size, code, _DTYPES[out_dtype], act, inner, out, n, x.data_ptr(), x_stride, w.data_ptr(), so, si, bias.data_ptr() if bias is not None else 0,
+        residual.data_ptr() if residual is not None else 0, strides[0], slope_at.data_ptr() if slope_at is not None else 0, strides[1], y.data_ptr(), out,
+        z.data_ptr() if keep else 0, out, work.data_ptr() if need else 0, need, st, device.index)
+    _check(lib.nomad_dense_product(a), "nomad_dense_product")
+    return (y, z) if keep else y
+
+
+def dense_gradient(dy, x, w, activation=None, z=None, need_dx=True, need_dw=True, bias=True, out_dtype=None, stream=None):
+    """nomad_dense_gradient: (dx [n, in], dW [out, in] of out_dtype, db [out] float32) of `dense_product` from dy [n, out]; with an
+    activation z is what keep=True returned.  What is not needed is None (db comes with dW); the residual's gradient is dy."""
+    device = x.device
+    _on(device, dy, w, z)
+    code, act = _dtype(x, "x"), _activation(activation)
+    n, columns, x_stride = _rows(x, "x")
+    out, inner, so, si = _weights(w, x.dtype, columns)
+    if dy.dtype != x.dtype or _matrix(dy, "dy")[0] != n:
+        raise ValueError(f"dy must be [{n}, {out}] of {x.dtype}")
+    dy_stride, z_stride = _rows(dy, "dy", out)[2], 0
+    if act:
+        if z is None or z.dtype != x.dtype or _matrix(z, "z")[0] != n:
+            raise ValueError(f"with an activation z must be [{n}, {out}] of {x.dtype}")
+        z_stride = _rows(z, "z", out)[2]
+    if not need_dx and not need_dw:
+        raise ValueError("neither gradient is asked for")
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    if out_dtype not in (x.dtype, torch.float32):
+        raise ValueError("out_dtype must be x's type or float32")
+    lib = load_library()
+    dx = torch.empty(n, inner, dtype=x.dtype, device=device) if need_dx else None
+    dw = torch.empty(out, inner, dtype=out_dtype, device=device) if need_dw else None
+    db = torch.empty(out, dtype=torch.float32, device=device) if need_dw and bias else None
+    need = lib.nomad_dense_gradient_workspace(n, inner, out, code, act)
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    st = _stream(device, stream, (dy, x, w, z if act else None, dx, dw, db, work))
+    pointer = lambda t: t.data_ptr() if t is not None else 0   # noqa: E731
+    a = binding.DENSE_GRADIENT_ARGS.pack(
+        binding.DENSE_GRADIENT_ARGS.size, code, _DTYPES[out_dtype], act, inner, out, n, dy.data_ptr(), dy_stride, z.data_ptr() if act else 0, z_stride, x.data_ptr(), x_stride,
+        w.data_ptr(), so, si, pointer(dx), inner, pointer(dw), pointer(db), pointer(work), need, st, device.index)
+    _check(lib.nomad_dense_gradient(a), "nomad_dense_gradient")
+    return dx, dw, db
+
+
 def combine(values, slots, weights=None, stream=None):
     """nomad_combine: y_i = sum_j weights[i, j] values[slots[i, j]] (weights None: ones)."""
     device = values.device
@@ -281,6 +457,39 @@ def combine_gradient(dy, values, slots, weights=None, order=None, need_dvalues=T
         weights.data_ptr() if weights is not None else None, n, k, dvalues.data_ptr() if need_dvalues else None,
         dweights.data_ptr() if need_dweights else None, device.index, st or None), "nomad_combine_gradient")
     return dvalues, dweights
+
+
+def gradient_norm(grads, max_norm=math.inf, grad_scale=None, stream=None):
+    """nomad_gradient_norm: (norm, scale), float32 tensors of one element on the GPU: the norm of all tensors together, and the factor that brings it
+    to max_norm at most, as `adamw_step` takes it (grad_scale).  grad_scale: None, or a factor that the gradients have yet to be multiplied
+    by, which norm and scale then contain."""
+    grads = list(grads)
+    if not grads:
+        raise ValueError("there are no gradients")
+    if not _all_tensors(grads):
+        raise ValueError("gradients must be tensors")
+    device = grads[0].device
+    _on(device, grad_scale)
+    if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
+        raise ValueError("grad_scale must be one float32 element")
+    max_norm = float(max_norm)
+    if not max_norm >= 0.0:
+        raise ValueError("max_norm must not be negative")
+    if set(map(torch.Tensor.get_device, grads)) != {device.index} or not all(map(torch.Tensor.is_contiguous, grads)):
+        raise ValueError(f"gradients must be contiguous and on {device}")
+    kinds = list(map(_DTYPES.get, map(_get_dtype, grads)))
+    if None in kinds:
+        raise ValueError("gradients must be float32, bfloat16 or float16")
+    lib, count = load_library(), len(grads)
+    flat = array.array("q", itertools.chain.from_iterable(zip(map(torch.Tensor.data_ptr, grads), map(torch.Tensor.numel, grads), kinds)))
+    out = torch.empty(2, dtype=torch.float32, device=device)
+    need = lib.nomad_gradient_norm_workspace(count)
+    work = torch.empty(need, dtype=torch.uint8, device=device)
+    st = _stream(device, stream, grads + [grad_scale, out, work])
+    at = out.data_ptr()
+    _check(lib.nomad_gradient_norm(flat.buffer_info()[0], count, max_norm, grad_scale.data_ptr() if grad_scale is not None else None, at, at + 4, work.data_ptr(), need,
+                                   device.index, st or None), "nomad_gradient_norm")
+    return out[:1], out[1:]
 
 
 class State8(NamedTuple):
