@@ -12,7 +12,8 @@ SOURCES = [os.path.join(_PKG, "csrc", "nomad.hip"), os.path.join(_PKG, "csrc", "
            os.path.join(_PKG, "csrc", "pca.hip"), os.path.join(_PKG, "csrc", "probes.hip"), os.path.join(_PKG, "csrc", "grouped.hip"), os.path.join(_PKG, "csrc", "grouped_bf16.hip"),
            os.path.join(_PKG, "csrc", "grouped_f16.hip"), os.path.join(_PKG, "csrc", "grouped_f32.hip"),
            os.path.join(_PKG, "csrc", "route.hip"), os.path.join(_PKG, "csrc", "adamw.hip"),
-           os.path.join(_PKG, "csrc", "scored.hip"), os.path.join(_PKG, "csrc", "norm.hip"), os.path.join(_PKG, "csrc", "dense.hip"),
+           os.path.join(_PKG, "csrc", "scored.hip"), os.path.join(_PKG, "csrc", "scored_bf16.hip"), os.path.join(_PKG, "csrc", "scored_f16.hip"),
+           os.path.join(_PKG, "csrc", "scored_f32.hip"), os.path.join(_PKG, "csrc", "norm.hip"), os.path.join(_PKG, "csrc", "dense.hip"),
            os.path.join(_PKG, "csrc", "dense_bf16.hip"), os.path.join(_PKG, "csrc", "dense_f16.hip"), os.path.join(_PKG, "csrc", "dense_f32.hip")]
 HEADERS = [os.path.join(_PKG, "csrc", "nomad_kernels.h"), os.path.join(_PKG, "csrc", "knn_kernels.h"),
            os.path.join(_PKG, "csrc", "knn_filter.h"), os.path.join(_PKG, "csrc", "knn_filter_kernel.h"), os.path.join(_PKG, "csrc", "filter_scale.h"),
@@ -23,7 +24,7 @@ HEADERS = [os.path.join(_PKG, "csrc", "nomad_kernels.h"), os.path.join(_PKG, "cs
            os.path.join(_PKG, "csrc", "edge_plan.h"), os.path.join(_PKG, "csrc", "exchange_kernels.h"),
            os.path.join(_PKG, "csrc", "run_kernels.h"), os.path.join(_PKG, "csrc", "field_kernels.h"), os.path.join(_PKG, "csrc", "small_kernels.h"), os.path.join(_PKG, "csrc", "kmeans_plan.h"),
            os.path.join(_PKG, "csrc", "grouped_kernels.h"), os.path.join(_PKG, "csrc", "grouped_launch.h"), os.path.join(_PKG, "csrc", "grouped_plan.h"), os.path.join(_PKG, "csrc", "route_kernels.h"), os.path.join(_PKG, "csrc", "adamw_kernels.h"), os.path.join(_PKG, "csrc", "device_scope.h"),
-           os.path.join(_PKG, "csrc", "route_launch.h"), os.path.join(_PKG, "csrc", "scored_kernels.h"), os.path.join(_PKG, "csrc", "norm_kernels.h"),
+           os.path.join(_PKG, "csrc", "route_launch.h"), os.path.join(_PKG, "csrc", "scored_kernels.h"), os.path.join(_PKG, "csrc", "scored_launch.h"), os.path.join(_PKG, "csrc", "norm_kernels.h"),
            os.path.join(_PKG, "csrc", "dense_kernels.h"), os.path.join(_PKG, "csrc", "dense_launch.h"), os.path.join(_PKG, "csrc", "dense_plan.h"),
            os.path.join(_ROOT, "include", "nomad.h")]
 

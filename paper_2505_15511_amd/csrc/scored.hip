@@ -4,71 +4,11 @@
 #include <cmath>
 
 #include "device_scope.h"
-#include "route_launch.h"
-#include "scored_kernels.h"
+#include "scored_launch.h"
 
 using namespace nomad_router;
 
 namespace {
-
-// lanes of a team where as many teams as there are groups (a power of two, at most all lanes) share the lanes of a row
-int32_t team_of(int32_t groups, int32_t lanes) {
-    int32_t teams = 1;
-    while (teams < groups && teams < lanes) teams *= 2;
-    return lanes / teams;
-}
-
-template <typename T, int LANES, int K>
-void launch_pick(ScoredArgs p, bool small, bool vec, hipStream_t st) {
-    p.team = team_of(p.groups, LANES);
-    p.open_team = team_of(p.top_groups, LANES);
-    if (small) {
-        const size_t lds = sizeof(int32_t) * (size_t)(p.r.n_experts + p.r.n * p.r.k);
-        if (vec) hipLaunchKernelGGL((k_scored_small<T, LANES, K, true>), dim3(1), dim3(kSmallThreads), lds, st, p);
-        else hipLaunchKernelGGL((k_scored_small<T, LANES, K, false>), dim3(1), dim3(kSmallThreads), lds, st, p);
-        return;
-    }
-    const dim3 grid((uint32_t)p.r.n_chunks), block(kPickThreads);
-    const size_t lds = sizeof(int32_t) * (size_t)p.r.n_experts;
-    if (vec) hipLaunchKernelGGL((k_scored_pick<T, LANES, K, true>), grid, block, lds, st, p);
-    else hipLaunchKernelGGL((k_scored_pick<T, LANES, K, false>), grid, block, lds, st, p);
-    launch_places(p.r, st);
-}
-template <typename T, int K>
-void launch_scored(const ScoredArgs& p, bool vec, hipStream_t st) {
-    const bool small = is_small(p.r.n, p.r.n_experts, p.r.k);
-    // as in nomad_route
-    const bool wide = p.r.n_experts > 512 || (small && p.r.n <= kSmallThreads / 64);
-    if (wide) launch_pick<T, 64, K>(p, small, vec, st);
-    else launch_pick<T, 16, K>(p, small, vec, st);
-}
-template <typename T>
-void launch_scored_k(const ScoredArgs& p, bool vec, hipStream_t st) {
-    if (p.r.k == 1) launch_scored<T, 1>(p, vec, st);
-    else if (p.r.k == 2) launch_scored<T, 2>(p, vec, st);
-    else if (p.r.k <= 4) launch_scored<T, 4>(p, vec, st);
-    else launch_scored<T, 8>(p, vec, st);
-}
-
-template <typename T, int K>
-void launch_gradient(const ScoredGradientArgs& p, bool vec, hipStream_t st) {
-    if (p.r.n_experts <= 512) {
-        const dim3 grid = grid_of((p.r.n + 15) / 16);
-        if (vec) hipLaunchKernelGGL((k_scored_gradient<T, 16, K, true>), grid, dim3(256), 0, st, p);
-        else hipLaunchKernelGGL((k_scored_gradient<T, 16, K, false>), grid, dim3(256), 0, st, p);
-    } else {
-        const dim3 grid = grid_of((p.r.n + 3) / 4);
-        if (vec) hipLaunchKernelGGL((k_scored_gradient<T, 64, K, true>), grid, dim3(256), 0, st, p);
-        else hipLaunchKernelGGL((k_scored_gradient<T, 64, K, false>), grid, dim3(256), 0, st, p);
-    }
-}
-template <typename T>
-void launch_gradient_k(const ScoredGradientArgs& p, bool vec, hipStream_t st) {
-    if (p.r.k == 1) launch_gradient<T, 1>(p, vec, st);
-    else if (p.r.k == 2) launch_gradient<T, 2>(p, vec, st);
-    else if (p.r.k <= 4) launch_gradient<T, 4>(p, vec, st);
-    else launch_gradient<T, 8>(p, vec, st);
-}
 
 bool is_scoring(const nomad_scoring* s, int32_t n_experts, int32_t k) {
     if (!s || s->struct_size != sizeof(nomad_scoring)) return false;
@@ -108,9 +48,9 @@ extern "C" int nomad_route_scored(const void* logits, int32_t dtype, int64_t n, 
     p.size = n_experts / p.groups;
     const int64_t size = size_of(dtype);
     const bool vec = by(logits, stride, size, 16) && p.size % (16 / size) == 0;
-    if (dtype == NOMAD_F32) launch_scored_k<float>(p, vec, st);
-    else if (dtype == NOMAD_BF16) launch_scored_k<__bf16>(p, vec, st);
-    else launch_scored_k<_Float16>(p, vec, st);
+    if (dtype == NOMAD_F32) scored_f32(p, vec, st);
+    else if (dtype == NOMAD_BF16) scored_bf16(p, vec, st);
+    else scored_f16(p, vec, st);
     KTRY(hipGetLastError());
     return NOMAD_OK;
 }
@@ -130,9 +70,9 @@ extern "C" int nomad_route_scored_gradient(const void* logits, int32_t dtype, in
     const int64_t size = size_of(dtype);
     const bool vec = (!over_all || by(logits, stride, size, 16)) && by(dlogits, n_experts, size, 16);
     hipStream_t st = (hipStream_t)stream;
-    if (dtype == NOMAD_F32) launch_gradient_k<float>(p, vec, st);
-    else if (dtype == NOMAD_BF16) launch_gradient_k<__bf16>(p, vec, st);
-    else launch_gradient_k<_Float16>(p, vec, st);
+    if (dtype == NOMAD_F32) scored_gradient_f32(p, vec, st);
+    else if (dtype == NOMAD_BF16) scored_gradient_bf16(p, vec, st);
+    else scored_gradient_f16(p, vec, st);
     KTRY(hipGetLastError());
     return NOMAD_OK;
 }

@@ -243,17 +243,13 @@ __device__ __forceinline__ bool choose(const T* row, const ScoredArgs& p, int su
         }
     }
     Largest<K, R> best;
-    if (p.groups == 1) {
-        each_of<T, VEC>(row, 0, n_experts, sub, LANES, [&](float v, uint32_t e) { best.take(s.of(v, e), e); });
-    } else {
-        const int teams = LANES / p.open_team, at = sub % p.open_team;
-        uint64_t left = open;
-        for (int skip = sub / p.open_team; skip > 0; --skip) left &= left - 1;
-        while (left) {
-            const int g = __builtin_ctzll(left);
-            each_of<T, VEC>(row, g * p.size, (g + 1) * p.size, at, p.open_team, [&](float v, uint32_t e) { best.take(s.of(v, e), e); });
-            for (int skip = teams; skip > 0; --skip) left &= left - 1;
-        }
+    const int open_teams = LANES / p.open_team, in_team = sub % p.open_team;
+    uint64_t left = open;
+    for (int skip = sub / p.open_team; skip > 0; --skip) left &= left - 1;
+    while (left) {
+        const int g = __builtin_ctzll(left);
+        each_of<T, VEC>(row, g * p.size, (g + 1) * p.size, in_team, p.open_team, [&](float v, uint32_t e) { best.take(s.of(v, e), e); });
+        for (int skip = open_teams; skip > 0; --skip) left &= left - 1;
     }
     R last = none;          // the k-th c
     R before = none;
@@ -289,15 +285,244 @@ __device__ __forceinline__ bool choose(const T* row, const ScoredArgs& p, int su
     return !FIRST || !any_of<LANES>(!sure, lane);
 }
 
+// ---- rows of up to 16 CAP experts, whose logits 16 lanes hold in registers, CAP each, and read once
+//
+// A lane's experts are of one group.  A sum c becomes a key of 32 bits: a whole number of steps above the smallest bias, below it the expert's
+// number, lower ones larger, so that comparing, sorting and taking the best are one instruction each.  (A step is 2^-24 or 2^-25 of the sums'
+// range.)  Without a bias the step is what is left of a logit's own order, all of it for logits of 16 bits.
+
+__device__ __forceinline__ void order(uint32_t& a, uint32_t& b) {   // the larger first
+    const uint32_t m = a > b ? a : b;
+    b = a > b ? b : a;
+    a = m;
+}
+template <int N>
+__device__ __forceinline__ void bitonic(uint32_t (&v)[N]) {   // a sequence that rises and falls -> descending
+#pragma unroll
+    for (int d = N / 2; d > 0; d /= 2)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if ((i & d) == 0) order(v[i], v[i + d]);
+}
+template <int N>
+__device__ __forceinline__ void sorted(uint32_t (&v)[N]) {   // descending
+#pragma unroll
+    for (int size = 2; size <= N; size *= 2)
+#pragma unroll
+        for (int d = size / 2; d > 0; d /= 2)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if ((i & d) == 0) {
+                    if ((i & size) == 0) order(v[i], v[i + d]);
+                    else order(v[i + d], v[i]);
+                }
+}
+// the L largest of N, descending
+template <int L, int N>
+__device__ __forceinline__ void largest(const uint32_t (&v)[N], uint32_t (&out)[L]) {
+#pragma unroll
+    for (int i = 0; i < L; ++i) out[i] = i < N ? v[i] : 0u;
+    sorted(out);
+#pragma unroll
+    for (int at = L; at < N; at += L) {
+        uint32_t more[L];
+#pragma unroll
+        for (int i = 0; i < L; ++i) more[i] = at + i < N ? v[at + i] : 0u;
+        sorted(more);
+#pragma unroll
+        for (int i = 0; i < L; ++i) out[i] = out[i] > more[L - 1 - i] ? out[i] : more[L - 1 - i];
+        bitonic(out);
+    }
+}
+
+__device__ __forceinline__ float power_of_e(float x) {   // for x <= 0, to a unit or two: what rounding x log2(e) loses is put back
+    const float power = x * 1.44269504f, rest = fmaf(x, 1.92596303e-8f, fmaf(x, 1.44269504f, -power)), e = __builtin_amdgcn_exp2f(power);
+    return x < -150.f ? 0.f : fmaf(e, rest * 0.69314718f, e);
+}
+
+template <typename T, int CAP, int K, bool VEC>
+struct Quick {
+    static constexpr int kLanes = 16, kEpc = VEC ? 16 / (int)sizeof(T) : 1, kChunks = CAP / kEpc;
+    static constexpr int kBits = CAP == 8 ? 7 : 8;                            // of an expert's number
+    static constexpr int kList = K == 2 ? 4 : 8;                              // a lane keeps: more than it can lose, but for K = 8
+    static constexpr float kSteps = (float)((1ull << (32 - kBits)) - 4);
+    struct alignas(VEC ? 16 : sizeof(T)) Chunk { T v[kEpc]; };
+    const ScoredArgs& p;
+    int sub, lane, group, from;            // from: of the group, the lane's first expert
+    int32_t first;                         // expert
+    bool by_logit, hopeless;
+    float bias[CAP];
+    float low, steps;                      // of the keys: the smallest sum there can be, steps a unit
+    float slack;                           // of a sum, beside its score's
+
+    __device__ __forceinline__ Quick(const ScoredArgs& args, int tid) : p(args) {
+        sub = tid % kLanes;
+        lane = tid & 63;
+        group = sub / p.team;
+        from = sub % p.team * kEpc;
+        first = group * p.size + from;
+        by_logit = p.bias == nullptr;
+        hopeless = false;
+        low = 0.f;
+        float high = 0.f;
+        if (!by_logit) {
+            low = INFINITY;
+            high = -INFINITY;
+            float wrong = 0.f;
+#pragma unroll
+            for (int i = 0; i < CAP; ++i) {
+                bias[i] = there(i) ? p.bias[number(i)] : 0.f;
+                if (there(i)) {
+                    low = fminf(low, bias[i]);
+                    high = fmaxf(high, bias[i]);
+                    wrong += bias[i] * 0.f;            // NaN where it is not a number
+                }
+            }
+            low = least_of<kLanes>(low);
+            high = most_of<kLanes>(high);
+            hopeless = fold<kLanes>(wrong, [](float a, float b) { return a + b; }) != 0.f || !(high - low < 1e30f);
+        }
+        steps = kSteps / (1.f + (high - low));
+        slack = 0x1p-21f * (fmaxf(fabsf(low), fabsf(high)) + 1.f);
+    }
+    __device__ __forceinline__ int32_t offset(int i) const { return (i / kEpc) * (p.team * kEpc) + i % kEpc; }
+    __device__ __forceinline__ int32_t number(int i) const { return first + offset(i); }
+    __device__ __forceinline__ bool there(int i) const { return group < p.groups && from + offset(i) < p.size; }
+
+    __device__ __forceinline__ void load(const T* row, Chunk (&raw)[kChunks]) const {
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j)
+            if (there(j * kEpc)) raw[j] = *(const Chunk*)(row + number(j * kEpc));
+    }
+
+    // The row's experts, best first, for every lane of the row; false: not to be told by 32 bits.  top, sum: of a softmax
+    __device__ __forceinline__ bool choose_quick(const T* row, const Chunk (&raw)[kChunks], int32_t (&expert)[K], float& top, float& sum) const {
+        const float none = -INFINITY;
+        float v[CAP];
+#pragma unroll
+        for (int i = 0; i < CAP; ++i) v[i] = there(i) ? value_of(raw[i / kEpc].v[i % kEpc]) : none;
+        bool sure = !hopeless;
+        top = none;
+        sum = 1.f;
+        float near = 0x1p-21f;
+        const bool two = p.groups > 1 && p.best == 2, scored = !by_logit || two;
+        float c[CAP];
+        if (!p.sigmoid && (scored || !p.r.normalize)) {
+#pragma unroll
+            for (int i = 0; i < CAP; ++i) top = fmaxf(top, v[i]);
+            top = most_of<kLanes>(top);
+            if (!(top < INFINITY)) sure = false;
+            const float base = top > none ? top : 0.f;
+            sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < CAP; ++i) {
+                c[i] = power_of_e(v[i] - base);
+                sum += c[i];
+            }
+            sum = fold<kLanes>(sum, [](float a, float b) { return a + b; });
+            const float inv = 1.f / sum;
+            near = inv * ((float)CAP + 32.f) * 0x1p-23f;
+#pragma unroll
+            for (int i = 0; i < CAP; ++i) c[i] *= inv;
+        } else if (scored) {
+#pragma unroll
+            for (int i = 0; i < CAP; ++i) c[i] = score_sigmoid(v[i], 0.f);
+        }
+        if (!by_logit)
+#pragma unroll
+            for (int i = 0; i < CAP; ++i) c[i] += bias[i];
+        bool open = true;
+        if (p.groups > 1) {
+            const bool as_logits = by_logit && !two;
+            float one = none, second = none, score;
+#pragma unroll
+            for (int i = 0; i < CAP; ++i) {
+                const float x = v[i] == none ? none : as_logits ? v[i] : c[i];
+                second = fmaxf(second, fminf(one, x));
+                one = fmaxf(one, x);
+            }
+            const auto join = [&](float other, float behind) {
+                second = fmaxf(fmaxf(second, behind), fminf(one, other));
+                one = fmaxf(one, other);
+            };
+            if (p.team > 1) join(moved<0xb1>(one), moved<0xb1>(second));
+            if (p.team > 2) join(moved<0x4e>(one), moved<0x4e>(second));
+            if (p.team > 4) join(moved<0x141>(one), moved<0x141>(second));
+            const bool both = p.best == 2 && second > none;
+            score = both ? one + second : one;
+            int ahead = 0;
+            const int base = lane - sub;
+            for (int g = 0; g < p.groups; ++g) {
+                const float other = __shfl(score, base + g * p.team);
+                ahead += other > score || (other == score && g < group) ? 1 : 0;
+            }
+            open = group < p.groups && score > none && ahead < p.top_groups;
+            if (!as_logits) {
+                const float lowest = least_of<kLanes>(open ? score : INFINITY), highest = most_of<kLanes>(open || group >= p.groups ? none : score);
+                if (highest > none && !(lowest - highest > 2.f * (near + slack * 2.f))) sure = false;
+            }
+        }
+        uint32_t key[CAP];
+#pragma unroll
+        for (int i = 0; i < CAP; ++i) {
+            uint32_t step;
+            if (by_logit) {
+                const uint32_t u = __float_as_uint(v[i]);
+                step = (u & 0x80000000u ? ~u : u | 0x80000000u) >> kBits;
+            } else {
+                step = (uint32_t)(fminf((c[i] - low) * steps, kSteps)) + 1u;
+            }
+            key[i] = open && v[i] > none ? step << kBits | ((1u << kBits) - 1u - (uint32_t)number(i)) : 0u;
+        }
+        uint32_t list[kList];
+        largest(key, list);
+        constexpr uint32_t mask = (1u << kBits) - 1u;
+        // steps within which keys may be in the wrong order
+        const uint32_t apart = by_logit ? 0u : (uint32_t)fminf((near + slack) * steps, 1e9f) + 2u;
+        const auto same = [&](uint32_t a, uint32_t b) {   // (a key's expert and another's: equal in every bit of logit and bias)
+            const int32_t ea = (int32_t)(mask - (a & mask)), eb = (int32_t)(mask - (b & mask));
+            return value_of(row[ea]) == value_of(row[eb]) && (by_logit || p.bias[ea] == p.bias[eb]);
+        };
+        const bool exact = by_logit && sizeof(T) == 2;    // equal steps are equal logits
+        uint32_t last = 0, before = 0;
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            expert[j] = -1;
+            if (j >= p.r.k) continue;
+            const uint32_t best = most_of<kLanes>(list[0]);
+            if (list[0] == best) {
+#pragma unroll
+                for (int i = 0; i + 1 < kList; ++i) list[i] = list[i + 1];
+                list[kList - 1] = best == 0 ? 0u : kList > K ? 0u : 1u;   // 1: something was let go there
+            }
+            if (best) expert[j] = (int32_t)(mask - (best & mask));
+            if (!exact && best && before && (before >> kBits) - (best >> kBits) <= apart && !same(before, best)) sure = false;
+            before = best;
+            last = j == p.r.k - 1 ? best : last;
+        }
+        if (!exact && last && list[0] && (last >> kBits) - (list[0] >> kBits) <= apart) {
+            bool all = true;
+#pragma unroll
+            for (int i = 0; i < kList; ++i) {
+                const bool close = list[i] != 0 && (last >> kBits) - (list[i] >> kBits) <= apart;
+                all = all && close;
+                if (close && !same(last, list[i])) sure = false;
+            }
+            if (all) sure = false;
+        }
+        if (kList == K && list[0] == 1u) sure = false;    // (a lane that has given all that it kept)
+        return !any_of<kLanes>(!sure, lane);
+    }
+};
+
 // log s up to what the chosen have in common, as a factor: s_j / s_m, for any logits
 __device__ __forceinline__ float sigmoid_ratio(float v, float m) {
     return expf(fminf(v, 0.f) - fminf(m, 0.f)) * ((1.f + expf(-fabsf(m))) / (1.f + expf(-fabsf(v))));
 }
 
-// One row: experts and, in lane j of the row for its j-th expert, the weight
-template <typename T, int LANES, int K, bool VEC>
-__device__ __forceinline__ float score_row(const T* row, const ScoredArgs& p, int sub, int32_t (&expert)[K]) {
-    if (!choose<float, T, LANES, K, VEC>(row, p, sub, expert)) (void)choose<double, T, LANES, K, VEC>(row, p, sub, expert);
+// A row's weights from its experts: lane j of the row gets the j-th (top, sum: of a softmax over all)
+template <typename T, int LANES, int K>
+__device__ __forceinline__ float weigh(const T* row, const ScoredArgs& p, int sub, const int32_t (&expert)[K], float top, float sum) {
     int32_t mine = -1;
 #pragma unroll
     for (int j = 0; j < K; ++j)
@@ -307,19 +532,64 @@ __device__ __forceinline__ float score_row(const T* row, const ScoredArgs& p, in
     if (p.r.normalize) {
         const float most = most_of<LANES>(v);
         if (mine >= 0) share = p.sigmoid ? sigmoid_ratio(v, most) : expf(v - most);
-        const float sum = fold<LANES>(share, [](float a, float b) { return a + b; });
-        if (mine >= 0) share /= sum;
+        const float chosen = fold<LANES>(share, [](float a, float b) { return a + b; });
+        if (mine >= 0) share /= chosen;
     } else if (p.sigmoid) {
         if (mine >= 0) share = expf(fminf(v, 0.f)) / (1.f + expf(-fabsf(v)));
-    } else {
-        float top = -INFINITY, sum = 0.f;
+    } else if (mine >= 0) {
+        share = expf(v - top) / sum;
+    }
+    return p.scale * share;
+}
+
+// One row: experts and, in lane j of the row for its j-th expert, the weight
+template <typename T, int LANES, int K, bool VEC>
+__device__ __forceinline__ float score_row(const T* row, const ScoredArgs& p, int sub, int32_t (&expert)[K]) {
+    if (!choose<float, T, LANES, K, VEC>(row, p, sub, expert)) (void)choose<double, T, LANES, K, false>(row, p, sub, expert);
+    float top = -INFINITY, sum = 0.f;
+    if (!p.sigmoid && !p.r.normalize) {
         each_of<T, VEC>(row, 0, p.r.n_experts, sub, LANES, [&](float x, uint32_t) { top = fmaxf(top, x); });
         top = most_of<LANES>(top);
         each_of<T, VEC>(row, 0, p.r.n_experts, sub, LANES, [&](float x, uint32_t) { sum += expf(x - top); });
         sum = fold<LANES>(sum, [](float a, float b) { return a + b; });
-        if (mine >= 0) share = expf(v - top) / sum;
     }
-    return p.scale * share;
+    return weigh<T, LANES, K>(row, p, sub, expert, top, sum);
+}
+
+// Chunks of rows as in k_route_pick, sixteen lanes a row; a lane asks for its next row before it looks at this one
+constexpr int kQuickThreads = 512;
+template <typename T, int CAP, int K, bool VEC>
+__global__ void __launch_bounds__(kQuickThreads) k_scored_quick(ScoredArgs p) {
+    typedef Quick<T, CAP, K, VEC> Row;
+    __shared__ int32_t tally[16 * CAP];
+    const int tid = threadIdx.x, sub = tid % 16;
+    if (tid < p.r.n_experts) tally[tid] = 0;
+    __syncthreads();
+    const Row q(p, tid);
+    const int64_t first = (int64_t)blockIdx.x * p.r.chunk, stop = first + p.r.chunk < p.r.n ? first + p.r.chunk : p.r.n;
+    int64_t i = first + tid / 16;
+    typename Row::Chunk raw[Row::kChunks], ahead[Row::kChunks];
+    if (i < stop) q.load((const T*)p.r.logits + i * p.r.stride, raw);
+    for (; i < stop; i += kQuickThreads / 16) {
+        const T* row = (const T*)p.r.logits + i * p.r.stride;
+        const int64_t next = i + kQuickThreads / 16;
+        if (next < stop) q.load((const T*)p.r.logits + next * p.r.stride, ahead);
+        int32_t expert[K];
+        float top, sum;
+        if (!q.choose_quick(row, raw, expert, top, sum)) (void)choose<double, T, 16, K, false>(row, p, sub, expert);
+        const float weight = weigh<T, 16, K>(row, p, sub, expert, top, sum);
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+            if (j < p.r.k && sub == j) {
+                p.r.experts[i * p.r.k + j] = expert[j];
+                p.r.weights[i * p.r.k + j] = weight;
+                if (expert[j] >= 0) atomicAdd(&tally[expert[j]], 1);
+            }
+#pragma unroll
+        for (int j = 0; j < Row::kChunks; ++j) raw[j] = ahead[j];
+    }
+    __syncthreads();
+    if (tid < p.r.n_experts) p.r.counts[(int64_t)blockIdx.x * p.r.n_experts + tid] = tally[tid];
 }
 
 template <typename T, int LANES, int K, bool VEC>
@@ -441,7 +711,7 @@ __global__ void __launch_bounds__(256) k_scored_gradient(ScoredGradientArgs p) {
 }
 
 // bias + rate where an expert has fewer rows than the mean, - rate where it has more
-__global__ void __launch_bounds__(256) k_balance_bias(const float* bias, const int32_t* offsets, int32_t n_experts, float rate, float* out) {
+static __global__ void __launch_bounds__(256) k_balance_bias(const float* bias, const int32_t* offsets, int32_t n_experts, float rate, float* out) {
     const int32_t e = blockIdx.x * 256 + threadIdx.x;
     if (e >= n_experts) return;
     const int64_t off = (int64_t)offsets[n_experts] - ((int64_t)offsets[e + 1] - offsets[e]) * n_experts;

@@ -1,0 +1,73 @@
+// Launches of routing by scores for one element type (each type has a source file of its own: they compile side by side).
+#pragma once
+#include "route_launch.h"
+#include "scored_kernels.h"
+
+namespace nomad_router {
+
+void scored_f32(const ScoredArgs& p, bool vec, hipStream_t st);
+void scored_bf16(const ScoredArgs& p, bool vec, hipStream_t st);
+void scored_f16(const ScoredArgs& p, bool vec, hipStream_t st);
+void scored_gradient_f32(const ScoredGradientArgs& p, bool vec, hipStream_t st);
+void scored_gradient_bf16(const ScoredGradientArgs& p, bool vec, hipStream_t st);
+void scored_gradient_f16(const ScoredGradientArgs& p, bool vec, hipStream_t st);
+
+// lanes of a team where as many teams as there are groups (a power of two, at most all lanes) share the lanes of a row
+inline int32_t team_of(int32_t groups, int32_t lanes) {
+    int32_t teams = 1;
+    while (teams < groups && teams < lanes) teams *= 2;
+    return lanes / teams;
+}
+// experts a lane of sixteen holds, where every lane has those of one group
+inline int32_t held_by_a_lane(const ScoredArgs& p, int32_t size, bool vec) {
+    const int32_t epc = vec ? 16 / size : 1, team = team_of(p.groups, 16);
+    return p.groups > 16 ? 1 << 30 : (p.size + team * epc - 1) / (team * epc) * epc;
+}
+
+template <typename T, int CAP, int K>
+void launch_quick(const ScoredArgs& p, bool vec, hipStream_t st) {
+    const dim3 grid((uint32_t)p.r.n_chunks), block(kQuickThreads);
+    if (vec) hipLaunchKernelGGL((k_scored_quick<T, CAP, K, true>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((k_scored_quick<T, CAP, K, false>), grid, block, 0, st, p);
+}
+template <typename T>
+void launch_scored(ScoredArgs p, bool vec, hipStream_t st) {
+    const int32_t held = held_by_a_lane(p, (int32_t)sizeof(T), vec);
+    const bool small = is_small(p.r.n, p.r.n_experts, p.r.k), quick = !small && held <= 16;
+    const int32_t lanes = quick || (small && p.r.n_experts <= 512) ? 16 : 64;
+    p.team = team_of(p.groups, lanes);
+    p.open_team = team_of(p.top_groups, lanes);
+    if (small) {
+        const size_t lds = sizeof(int32_t) * (size_t)(p.r.n_experts + p.r.n * p.r.k);
+        if (lanes == 16) hipLaunchKernelGGL((k_scored_small<T, 16, 8, false>), dim3(1), dim3(kSmallThreads), lds, st, p);
+        else hipLaunchKernelGGL((k_scored_small<T, 64, 8, false>), dim3(1), dim3(kSmallThreads), lds, st, p);
+        return;
+    }
+    if (quick) {
+        if (held <= 8 && p.r.k <= 2) launch_quick<T, 8, 2>(p, vec, st);
+        else if (held <= 8) launch_quick<T, 8, 8>(p, vec, st);
+        else if (p.r.k <= 2) launch_quick<T, 16, 2>(p, vec, st);
+        else launch_quick<T, 16, 8>(p, vec, st);
+    } else {
+        const dim3 grid((uint32_t)p.r.n_chunks), block(kPickThreads);
+        const size_t lds = sizeof(int32_t) * (size_t)p.r.n_experts;
+        if (vec) hipLaunchKernelGGL((k_scored_pick<T, 64, 8, true>), grid, block, lds, st, p);
+        else hipLaunchKernelGGL((k_scored_pick<T, 64, 8, false>), grid, block, lds, st, p);
+    }
+    launch_places(p.r, st);
+}
+
+template <typename T, int K, int LANES>
+void launch_scored_gradient(const ScoredGradientArgs& p, bool vec, hipStream_t st) {
+    const dim3 grid = grid_of((p.r.n + 256 / LANES - 1) / (256 / LANES));
+    if (vec) hipLaunchKernelGGL((k_scored_gradient<T, LANES, K, true>), grid, dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((k_scored_gradient<T, LANES, K, false>), grid, dim3(256), 0, st, p);
+}
+template <typename T>
+void launch_scored_gradient_type(const ScoredGradientArgs& p, bool vec, hipStream_t st) {
+    if (p.r.n_experts <= 512 && p.r.k <= 2) launch_scored_gradient<T, 2, 16>(p, vec, st);
+    else if (p.r.n_experts <= 512) launch_scored_gradient<T, 8, 16>(p, vec, st);
+    else launch_scored_gradient<T, 8, 64>(p, vec, st);
+}
+
+}  // namespace nomad_router
