@@ -12,7 +12,7 @@ inline bool by(const void* p, int64_t stride, int64_t size, int64_t bytes) { ret
 
 // Rows a chunk of the counts: their scan walks the chunks of an expert, so there are about a thousand at most, and no fewer rows
 // in one than keep the counts well below the logits
-inline int64_t chunk_rows(int64_t n) { return std::max<int64_t>(256, (n + 1023) / 1024); }
+inline int64_t chunk_rows(int64_t n) { return std::max<int64_t>(64, (n + 1023) / 1024); }
 // One workgroup does it all where the logits are few (a row of 256: 4.4 us, the three kernels of the other form 12.4; 100 rows of 50: 6.4 against 40)
 // and its counters and slots fit the 64 KB of LDS that a launch has without asking
 inline bool is_small(int64_t n, int32_t n_experts, int32_t k) { return n * n_experts <= 32768 && n <= 1024 && n_experts + n * k <= 16384; }

@@ -340,19 +340,20 @@ __device__ __forceinline__ float power_of_e(float x) {   // for x <= 0, to a uni
     return x < -150.f ? 0.f : fmaf(e, rest * 0.69314718f, e);
 }
 
-template <typename T, int CAP, int K, bool VEC>
+template <typename T, int CAP, int K, bool VEC, bool GROUPED>
 struct Quick {
     static constexpr int kLanes = 16, kEpc = VEC ? 16 / (int)sizeof(T) : 1, kChunks = CAP / kEpc;
     static constexpr int kBits = CAP == 8 ? 7 : 8;                            // of an expert's number
     static constexpr int kList = K == 2 ? 4 : 8;                              // a lane keeps: more than it can lose, but for K = 8
-    static constexpr float kSteps = (float)((1ull << (32 - kBits)) - 4);
+    static constexpr float kSteps = (float)((1ull << (32 - kBits)) - 64);     // (rounding takes a key a few steps further)
     struct alignas(VEC ? 16 : sizeof(T)) Chunk { T v[kEpc]; };
     const ScoredArgs& p;
     int sub, lane, group, from;            // from: of the group, the lane's first expert
     int32_t first;                         // expert
-    bool by_logit, hopeless;
-    float bias[CAP];
-    float low, steps;                      // of the keys: the smallest sum there can be, steps a unit
+    bool hopeless;
+    float low;                             // the smallest bias
+    float steps;                           // of the keys: a unit's
+    float start[CAP];                      // steps of the bias above the smallest one
     float slack;                           // of a sum, beside its score's
 
     __device__ __forceinline__ Quick(const ScoredArgs& args, int tid) : p(args) {
@@ -361,34 +362,43 @@ struct Quick {
         group = sub / p.team;
         from = sub % p.team * kEpc;
         first = group * p.size + from;
-        by_logit = p.bias == nullptr;
         hopeless = false;
         low = 0.f;
         float high = 0.f;
-        if (!by_logit) {
+#pragma unroll
+        for (int i = 0; i < CAP; ++i) start[i] = 0.f;
+        if (p.bias) {
             low = INFINITY;
             high = -INFINITY;
             float wrong = 0.f;
 #pragma unroll
+            for (int i = 0; i < CAP; ++i) start[i] = p.bias[there(i) ? number(i) : 0];   // (all on their way at once)
+#pragma unroll
             for (int i = 0; i < CAP; ++i) {
-                bias[i] = there(i) ? p.bias[number(i)] : 0.f;
-                if (there(i)) {
-                    low = fminf(low, bias[i]);
-                    high = fmaxf(high, bias[i]);
-                    wrong += bias[i] * 0.f;            // NaN where it is not a number
-                }
+                low = fminf(low, start[i]);
+                high = fmaxf(high, start[i]);
+                wrong += start[i] * 0.f;               // NaN where it is not a number
             }
             low = least_of<kLanes>(low);
             high = most_of<kLanes>(high);
             hopeless = fold<kLanes>(wrong, [](float a, float b) { return a + b; }) != 0.f || !(high - low < 1e30f);
         }
         steps = kSteps / (1.f + (high - low));
+#pragma unroll
+        for (int i = 0; i < CAP; ++i) start[i] = (start[i] - low) * steps + 1.f;
         slack = 0x1p-21f * (fmaxf(fabsf(low), fabsf(high)) + 1.f);
     }
     __device__ __forceinline__ int32_t offset(int i) const { return (i / kEpc) * (p.team * kEpc) + i % kEpc; }
     __device__ __forceinline__ int32_t number(int i) const { return first + offset(i); }
     __device__ __forceinline__ bool there(int i) const { return group < p.groups && from + offset(i) < p.size; }
 
+    // what a lane's places hold that no expert has
+    __device__ __forceinline__ static void clear(Chunk (&raw)[kChunks]) {
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j)
+#pragma unroll
+            for (int i = 0; i < kEpc; ++i) raw[j].v[i] = (T)-INFINITY;
+    }
     __device__ __forceinline__ void load(const T* row, Chunk (&raw)[kChunks]) const {
 #pragma unroll
         for (int j = 0; j < kChunks; ++j)
@@ -400,18 +410,18 @@ struct Quick {
         const float none = -INFINITY;
         float v[CAP];
 #pragma unroll
-        for (int i = 0; i < CAP; ++i) v[i] = there(i) ? value_of(raw[i / kEpc].v[i % kEpc]) : none;
+        for (int i = 0; i < CAP; ++i) v[i] = fmaxf((float)raw[i / kEpc].v[i % kEpc], none);   // (a NaN is -inf)
         bool sure = !hopeless;
         top = none;
         sum = 1.f;
         float near = 0x1p-21f;
-        const bool two = p.groups > 1 && p.best == 2, scored = !by_logit || two;
+        const bool by_logit = p.bias == nullptr, two = GROUPED && p.best == 2, scored = !by_logit || two;
         float c[CAP];
         if (!p.sigmoid && (scored || !p.r.normalize)) {
 #pragma unroll
             for (int i = 0; i < CAP; ++i) top = fmaxf(top, v[i]);
             top = most_of<kLanes>(top);
-            if (!(top < INFINITY)) sure = false;
+            if (scored && !(top < INFINITY)) sure = false;
             const float base = top > none ? top : 0.f;
             sum = 0.f;
 #pragma unroll
@@ -430,9 +440,9 @@ struct Quick {
         }
         if (!by_logit)
 #pragma unroll
-            for (int i = 0; i < CAP; ++i) c[i] += bias[i];
+            for (int i = 0; i < CAP; ++i) c[i] = fmaf(c[i], steps, start[i]);   // (the sum, in steps)
         bool open = true;
-        if (p.groups > 1) {
+        if (GROUPED) {
             const bool as_logits = by_logit && !two;
             float one = none, second = none, score;
 #pragma unroll
@@ -450,6 +460,7 @@ struct Quick {
             if (p.team > 4) join(moved<0x141>(one), moved<0x141>(second));
             const bool both = p.best == 2 && second > none;
             score = both ? one + second : one;
+            if (!by_logit) score = both ? fmaf(score - 2.f, 1.f / steps, 2.f * low) : fmaf(score - 1.f, 1.f / steps, low);
             int ahead = 0;
             const int base = lane - sub;
             for (int g = 0; g < p.groups; ++g) {
@@ -462,21 +473,27 @@ struct Quick {
                 if (highest > none && !(lowest - highest > 2.f * (near + slack * 2.f))) sure = false;
             }
         }
+        constexpr uint32_t mask = (1u << kBits) - 1u;
         uint32_t key[CAP];
+        if (by_logit) {
 #pragma unroll
-        for (int i = 0; i < CAP; ++i) {
-            uint32_t step;
-            if (by_logit) {
-                const uint32_t u = __float_as_uint(v[i]);
-                step = (u & 0x80000000u ? ~u : u | 0x80000000u) >> kBits;
-            } else {
-                step = (uint32_t)(fminf((c[i] - low) * steps, kSteps)) + 1u;
+            for (int i = 0; i < CAP; ++i) {
+                const uint32_t u = __float_as_uint(v[i] + 0.f);   // (both zeros are the same number)
+                key[i] = u & 0x80000000u ? ~u : u | 0x80000000u;
             }
-            key[i] = open && v[i] > none ? step << kBits | ((1u << kBits) - 1u - (uint32_t)number(i)) : 0u;
+#pragma unroll
+            for (int i = 0; i < CAP; ++i) key[i] = (key[i] & ~mask) | (mask - (uint32_t)number(i));
+        } else {
+#pragma unroll
+            for (int i = 0; i < CAP; ++i) key[i] = (uint32_t)c[i] << kBits | (mask - (uint32_t)number(i));
         }
+#pragma unroll
+        for (int i = 0; i < CAP; ++i) key[i] = v[i] > none ? key[i] : 0u;
         uint32_t list[kList];
         largest(key, list);
-        constexpr uint32_t mask = (1u << kBits) - 1u;
+        if (GROUPED)
+#pragma unroll
+            for (int i = 0; i < kList; ++i) list[i] = open ? list[i] : 0u;
         // steps within which keys may be in the wrong order
         const uint32_t apart = by_logit ? 0u : (uint32_t)fminf((near + slack) * steps, 1e9f) + 2u;
         const auto same = [&](uint32_t a, uint32_t b) {   // (a key's expert and another's: equal in every bit of logit and bias)
@@ -510,14 +527,14 @@ struct Quick {
             }
             if (all) sure = false;
         }
-        if (kList == K && list[0] == 1u) sure = false;    // (a lane that has given all that it kept)
+        if (!exact && kList == K && list[0] == 1u) sure = false;    // (a lane that has given all that it kept)
         return !any_of<kLanes>(!sure, lane);
     }
 };
 
 // log s up to what the chosen have in common, as a factor: s_j / s_m, for any logits
 __device__ __forceinline__ float sigmoid_ratio(float v, float m) {
-    return expf(fminf(v, 0.f) - fminf(m, 0.f)) * ((1.f + expf(-fabsf(m))) / (1.f + expf(-fabsf(v))));
+    return power_of_e(fminf(v, 0.f) - fminf(m, 0.f)) * ((1.f + power_of_e(-fabsf(m))) * __builtin_amdgcn_rcpf(1.f + power_of_e(-fabsf(v))));
 }
 
 // A row's weights from its experts: lane j of the row gets the j-th (top, sum: of a softmax over all)
@@ -531,21 +548,21 @@ __device__ __forceinline__ float weigh(const T* row, const ScoredArgs& p, int su
     float share = 0.f;
     if (p.r.normalize) {
         const float most = most_of<LANES>(v);
-        if (mine >= 0) share = p.sigmoid ? sigmoid_ratio(v, most) : expf(v - most);
+        if (mine >= 0) share = p.sigmoid ? sigmoid_ratio(v, most) : power_of_e(v - most);
         const float chosen = fold<LANES>(share, [](float a, float b) { return a + b; });
-        if (mine >= 0) share /= chosen;
+        if (mine >= 0) share *= __builtin_amdgcn_rcpf(chosen);
     } else if (p.sigmoid) {
-        if (mine >= 0) share = expf(fminf(v, 0.f)) / (1.f + expf(-fabsf(v)));
+        if (mine >= 0) share = power_of_e(fminf(v, 0.f)) * __builtin_amdgcn_rcpf(1.f + power_of_e(-fabsf(v)));
     } else if (mine >= 0) {
         share = expf(v - top) / sum;
     }
     return p.scale * share;
 }
 
-// One row: experts and, in lane j of the row for its j-th expert, the weight
-template <typename T, int LANES, int K, bool VEC>
+// One row: experts and, in lane j of the row for its j-th expert, the weight.  R = double: 32 bits have been tried
+template <typename R, typename T, int LANES, int K, bool VEC>
 __device__ __forceinline__ float score_row(const T* row, const ScoredArgs& p, int sub, int32_t (&expert)[K]) {
-    if (!choose<float, T, LANES, K, VEC>(row, p, sub, expert)) (void)choose<double, T, LANES, K, false>(row, p, sub, expert);
+    if (sizeof(R) == 8 || !choose<float, T, LANES, K, VEC>(row, p, sub, expert)) (void)choose<double, T, LANES, K, false>(row, p, sub, expert);
     float top = -INFINITY, sum = 0.f;
     if (!p.sigmoid && !p.r.normalize) {
         each_of<T, VEC>(row, 0, p.r.n_experts, sub, LANES, [&](float x, uint32_t) { top = fmaxf(top, x); });
@@ -556,11 +573,13 @@ __device__ __forceinline__ float score_row(const T* row, const ScoredArgs& p, in
     return weigh<T, LANES, K>(row, p, sub, expert, top, sum);
 }
 
-// Chunks of rows as in k_route_pick, sixteen lanes a row; a lane asks for its next row before it looks at this one
+// Chunks of rows as in k_route_pick, sixteen lanes a row; a lane asks for its next row before it looks at this one.  Rows that 32 bits do not tell
+// apart are marked and left to k_scored_rest: 64 bits in here took the registers of every row (500,000 rows of 256 in float32: 217 us).
 constexpr int kQuickThreads = 512;
-template <typename T, int CAP, int K, bool VEC>
+constexpr int32_t kLeft = -2;
+template <typename T, int CAP, int K, bool VEC, bool GROUPED>
 __global__ void __launch_bounds__(kQuickThreads) k_scored_quick(ScoredArgs p) {
-    typedef Quick<T, CAP, K, VEC> Row;
+    typedef Quick<T, CAP, K, VEC, GROUPED> Row;
     __shared__ int32_t tally[16 * CAP];
     const int tid = threadIdx.x, sub = tid % 16;
     if (tid < p.r.n_experts) tally[tid] = 0;
@@ -569,6 +588,8 @@ __global__ void __launch_bounds__(kQuickThreads) k_scored_quick(ScoredArgs p) {
     const int64_t first = (int64_t)blockIdx.x * p.r.chunk, stop = first + p.r.chunk < p.r.n ? first + p.r.chunk : p.r.n;
     int64_t i = first + tid / 16;
     typename Row::Chunk raw[Row::kChunks], ahead[Row::kChunks];
+    Row::clear(raw);
+    Row::clear(ahead);
     if (i < stop) q.load((const T*)p.r.logits + i * p.r.stride, raw);
     for (; i < stop; i += kQuickThreads / 16) {
         const T* row = (const T*)p.r.logits + i * p.r.stride;
@@ -576,20 +597,53 @@ __global__ void __launch_bounds__(kQuickThreads) k_scored_quick(ScoredArgs p) {
         if (next < stop) q.load((const T*)p.r.logits + next * p.r.stride, ahead);
         int32_t expert[K];
         float top, sum;
-        if (!q.choose_quick(row, raw, expert, top, sum)) (void)choose<double, T, 16, K, false>(row, p, sub, expert);
+        const bool sure = q.choose_quick(row, raw, expert, top, sum);
         const float weight = weigh<T, 16, K>(row, p, sub, expert, top, sum);
+        int32_t mine = kLeft;
 #pragma unroll
         for (int j = 0; j < K; ++j)
-            if (j < p.r.k && sub == j) {
-                p.r.experts[i * p.r.k + j] = expert[j];
-                p.r.weights[i * p.r.k + j] = weight;
-                if (expert[j] >= 0) atomicAdd(&tally[expert[j]], 1);
-            }
+            if (sure && sub == j) mine = expert[j];
+        if (sub < p.r.k) {
+            p.r.experts[i * p.r.k + sub] = mine;
+            p.r.weights[i * p.r.k + sub] = weight;
+            if (mine >= 0) atomicAdd(&tally[mine], 1);
+        }
 #pragma unroll
         for (int j = 0; j < Row::kChunks; ++j) raw[j] = ahead[j];
     }
     __syncthreads();
     if (tid < p.r.n_experts) p.r.counts[(int64_t)blockIdx.x * p.r.n_experts + tid] = tally[tid];
+}
+
+// The rows that k_scored_quick has marked, 64 bits for all of a row's experts; the chunk's counts with theirs
+constexpr int kRestThreads = 256;
+template <typename T>
+__global__ void __launch_bounds__(kRestThreads) k_scored_rest(ScoredArgs p) {
+    __shared__ int32_t rows[kRestThreads], left;
+    const int tid = threadIdx.x, sub = tid % 64;   // (a wavefront a row: there are few, and the way of one is what the kernel takes)
+    const int64_t first = (int64_t)blockIdx.x * p.r.chunk, stop = first + p.r.chunk < p.r.n ? first + p.r.chunk : p.r.n;
+    for (int64_t i0 = first; i0 < stop; i0 += kRestThreads) {
+        if (tid == 0) left = 0;
+        __syncthreads();
+        if (i0 + tid < stop && p.r.experts[(i0 + tid) * p.r.k] == kLeft) rows[atomicAdd(&left, 1)] = tid;
+        __syncthreads();
+        const int32_t all = left;
+        for (int32_t at = tid / 64; at < all; at += kRestThreads / 64) {   // (in any order: each row by itself)
+            const int64_t i = i0 + rows[at];
+            int32_t expert[kMaxK];
+            const float weight = score_row<double, T, 64, kMaxK, false>((const T*)p.r.logits + i * p.r.stride, p, sub, expert);
+            int32_t mine = -1;
+#pragma unroll
+            for (int j = 0; j < kMaxK; ++j)
+                if (sub == j) mine = expert[j];
+            if (sub < p.r.k) {
+                p.r.experts[i * p.r.k + sub] = mine;
+                p.r.weights[i * p.r.k + sub] = weight;
+                if (mine >= 0) atomicAdd(&p.r.counts[(int64_t)blockIdx.x * p.r.n_experts + mine], 1);
+            }
+        }
+        __syncthreads();
+    }
 }
 
 template <typename T, int LANES, int K, bool VEC>
@@ -601,7 +655,7 @@ __global__ void __launch_bounds__(kPickThreads) k_scored_pick(ScoredArgs p) {
     const int64_t first = (int64_t)blockIdx.x * p.r.chunk, stop = first + p.r.chunk < p.r.n ? first + p.r.chunk : p.r.n;
     for (int64_t i = first + tid / LANES; i < stop; i += kPickThreads / LANES) {
         int32_t expert[K];
-        const float weight = score_row<T, LANES, K, VEC>((const T*)p.r.logits + i * p.r.stride, p, sub, expert);
+        const float weight = score_row<float, T, LANES, K, VEC>((const T*)p.r.logits + i * p.r.stride, p, sub, expert);
 #pragma unroll
         for (int j = 0; j < K; ++j)
             if (j < p.r.k && sub == j) {
@@ -623,7 +677,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_scored_small(ScoredArgs p) {
     __syncthreads();
     for (int64_t i = tid / LANES; i < p.r.n; i += kSmallThreads / LANES) {
         int32_t expert[K];
-        const float weight = score_row<T, LANES, K, VEC>((const T*)p.r.logits + i * p.r.stride, p, sub, expert);
+        const float weight = score_row<float, T, LANES, K, VEC>((const T*)p.r.logits + i * p.r.stride, p, sub, expert);
 #pragma unroll
         for (int j = 0; j < K; ++j)
             if (j < p.r.k && sub == j) {
@@ -708,6 +762,39 @@ __global__ void __launch_bounds__(256) k_scored_gradient(ScoredGradientArgs p) {
         }
         store_chunk<T, VEC>(out + c, part);
     }
+}
+
+// The same where a row's gradient is 0 but for its experts: lane j of a row has the j-th, puts it into the row in LDS, and the row leaves whole (a
+// comparison of every expert with every chosen one took 300,000 rows of 256 in bfloat16, k = 8, 114 us)
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) k_scored_gradient_rows(ScoredGradientArgs p) {
+    extern __shared__ uint4 rows[];
+    constexpr int epc = VEC ? 16 / (int)sizeof(T) : 1;
+    const int sub = threadIdx.x % 16, line = threadIdx.x / 16;
+    const int64_t i = block_number() * 16 + line;
+    if (i >= p.r.n) return;   // (whole rows leave, and a row's lanes are of one wavefront: nothing here waits for others)
+    const int32_t chunks = (p.r.n_experts * (int32_t)sizeof(T) + 15) / 16;
+    uint4* held = rows + line * chunks;
+    int32_t expert = -1;
+    float weight = 0.f, given = 0.f;
+    if (sub < p.r.k) {
+        const int64_t at = i * p.r.k + sub;
+        expert = p.r.experts[at];
+        weight = p.r.weights[at];
+        given = p.r.dweights[at];
+        if (expert >= p.r.n_experts) expert = -1;
+    }
+    for (int32_t c = sub; c < chunks; c += 16) held[c] = make_uint4(0, 0, 0, 0);
+    const float inner = fold<16>(expert < 0 ? 0.f : weight * given, [](float a, float b) { return a + b; });
+    float value = weight * (given - inner * p.over);
+    if (expert >= 0 && p.sigmoid) value /= 1.f + expf(value_of(((const T*)p.r.logits)[i * p.r.stride + expert]));
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (expert >= 0) ((T*)held)[expert] = (T)value;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    T* out = (T*)p.r.dlogits + i * p.r.n_experts;
+    for (int32_t c = sub * epc; c < p.r.n_experts; c += 16 * epc) store_chunk<T, VEC>(out + c, (const T*)held + c);
 }
 
 // bias + rate where an expert has fewer rows than the mean, - rate where it has more

@@ -27,14 +27,21 @@ inline int32_t held_by_a_lane(const ScoredArgs& p, int32_t size, bool vec) {
 template <typename T, int CAP, int K>
 void launch_quick(const ScoredArgs& p, bool vec, hipStream_t st) {
     const dim3 grid((uint32_t)p.r.n_chunks), block(kQuickThreads);
-    if (vec) hipLaunchKernelGGL((k_scored_quick<T, CAP, K, true>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((k_scored_quick<T, CAP, K, false>), grid, block, 0, st, p);
+    if (p.groups > 1 && vec) hipLaunchKernelGGL((k_scored_quick<T, CAP, K, true, true>), grid, block, 0, st, p);
+    else if (p.groups > 1) hipLaunchKernelGGL((k_scored_quick<T, CAP, K, false, true>), grid, block, 0, st, p);
+    else if (vec) hipLaunchKernelGGL((k_scored_quick<T, CAP, K, true, false>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((k_scored_quick<T, CAP, K, false, false>), grid, block, 0, st, p);
+    if (!p.bias && sizeof(T) == 2 && (p.groups == 1 || p.best == 1)) return;   // (logits of 16 bits, which keys hold whole)
+    ScoredArgs rest = p;
+    rest.team = team_of(p.groups, 64);
+    rest.open_team = team_of(p.top_groups, 64);
+    hipLaunchKernelGGL((k_scored_rest<T>), grid, dim3(kRestThreads), 0, st, rest);
 }
 template <typename T>
 void launch_scored(ScoredArgs p, bool vec, hipStream_t st) {
     const int32_t held = held_by_a_lane(p, (int32_t)sizeof(T), vec);
     const bool small = is_small(p.r.n, p.r.n_experts, p.r.k), quick = !small && held <= 16;
-    const int32_t lanes = quick || (small && p.r.n_experts <= 512) ? 16 : 64;
+    const int32_t lanes = quick || (small && p.r.n > kSmallThreads / 64 && p.r.n_experts <= 512) ? 16 : 64;
     p.team = team_of(p.groups, lanes);
     p.open_team = team_of(p.top_groups, lanes);
     if (small) {
@@ -65,8 +72,12 @@ void launch_scored_gradient(const ScoredGradientArgs& p, bool vec, hipStream_t s
 }
 template <typename T>
 void launch_scored_gradient_type(const ScoredGradientArgs& p, bool vec, hipStream_t st) {
-    if (p.r.n_experts <= 512 && p.r.k <= 2) launch_scored_gradient<T, 2, 16>(p, vec, st);
-    else if (p.r.n_experts <= 512) launch_scored_gradient<T, 8, 16>(p, vec, st);
+    if (p.r.n_experts <= 512 && (p.sigmoid || p.r.normalize)) {
+        const dim3 grid = grid_of((p.r.n + 15) / 16);
+        const size_t lds = 16 * (((size_t)p.r.n_experts * sizeof(T) + 15) / 16 * 16);
+        if (vec) hipLaunchKernelGGL((k_scored_gradient_rows<T, true>), grid, dim3(256), lds, st, p);
+        else hipLaunchKernelGGL((k_scored_gradient_rows<T, false>), grid, dim3(256), lds, st, p);
+    } else if (p.r.n_experts <= 512) launch_scored_gradient<T, 8, 16>(p, vec, st);
     else launch_scored_gradient<T, 8, 64>(p, vec, st);
 }
 
