@@ -31,6 +31,12 @@ constexpr int kPlanUnits = 256;
 
 // Work space of a product: [parts][rows][columns] in float32 where there is more than one part
 int64_t part_bytes(const Plan& plan, int64_t rows, int64_t columns) { return plan.parts > 1 ? round16(plan.parts * rows * columns * (int64_t)sizeof(float)) : 0; }
+// and of whichever plan a product has: alignment and the order of W's strides, which the size does not know, have a say in it
+int64_t most_bytes(int64_t rows, int64_t columns, int64_t k, bool small) {
+    int64_t most = 0;
+    for (int way = 0; way < 4; ++way) most = std::max(most, part_bytes(plan(rows, columns, k, small, way & 1, way & 2, kPlanUnits), rows, columns));
+    return most;
+}
 // Where the sums go that are not finished where they are made: parts to work space, and float32 results of 16-bit operands to their place, where
 // what follows is done to them
 void place_sums(DenseArgs& p, Launch& l, void* work) {
@@ -54,17 +60,10 @@ void launch(int32_t dtype, const DenseArgs& p, const Launch& l, hipStream_t st) 
 
 }  // namespace
 
-// A plan must not depend on alignment where the work space does not know it: `whole` stands for large tiles, and a product that has none for
-// want of it has as many tiles as fill the device or more, and so one part either way.
 #pragma GCC visibility push(default)
 extern "C" int64_t nomad_dense_workspace(int64_t rows, int32_t in, int32_t out, int32_t dtype) {
     if (rows < 1 || in < 1 || out < 1 || !is_dtype(dtype) || rows > NOMAD_MAX_ROWS || in > NOMAD_MAX_COLUMNS || out > NOMAD_MAX_COLUMNS) return 0;
-    int64_t most = 0;
-    for (int few = 0; few < 2; ++few) {
-        const Plan l = plan(rows, out, in, size_of(dtype) == 2, few != 0, false, kPlanUnits);
-        most = std::max(most, part_bytes(l, rows, out));
-    }
-    return most;
+    return most_bytes(rows, out, in, size_of(dtype) == 2);
 }
 
 extern "C" int nomad_dense_product(const nomad_dense_args* args) {
@@ -122,9 +121,8 @@ extern "C" int nomad_dense_product(const nomad_dense_args* args) {
 extern "C" int64_t nomad_dense_gradient_workspace(int64_t rows, int32_t in, int32_t out, int32_t dtype, int32_t activation) {
     if (rows < 1 || in < 1 || out < 1 || !is_dtype(dtype) || rows > NOMAD_MAX_ROWS || in > NOMAD_MAX_COLUMNS || out > NOMAD_MAX_COLUMNS) return 0;
     const bool small = size_of(dtype) == 2;
-    const Plan dx = plan(rows, in, out, small, false, false, kPlanUnits), dw = plan(out, in, rows, small, false, false, kPlanUnits);
-    const int64_t products = std::max(part_bytes(dx, rows, in), part_bytes(dw, out, in));
-    if (activation == NOMAD_ACT_NONE) return products + (dw.parts > 1 ? round16(dw.parts * out * (int64_t)sizeof(float)) : 0);
+    const int64_t products = std::max(most_bytes(rows, in, out, small), most_bytes(out, in, rows, small));
+    if (activation == NOMAD_ACT_NONE) return products + round16(kMostParts * out * (int64_t)sizeof(float));
     return products + round16(rows * out * size_of(dtype)) + round16(plan_slope(rows, out, kPlanUnits).parts * out * (int64_t)sizeof(float));
 }
 
