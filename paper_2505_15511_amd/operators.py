@@ -477,11 +477,16 @@ def gradient_norm(grads, max_norm=math.inf, grad_scale=None, stream=None):
         raise ValueError("max_norm must not be negative")
     if set(map(torch.Tensor.get_device, grads)) != {device.index} or not all(map(torch.Tensor.is_contiguous, grads)):
         raise ValueError(f"gradients must be contiguous and on {device}")
-    kinds = list(map(_DTYPES.get, map(_get_dtype, grads)))
-    if None in kinds:
+    dtypes = set(map(_get_dtype, grads))
+    if not dtypes <= _DTYPES.keys():
         raise ValueError("gradients must be float32, bfloat16 or float16")
     lib, count = load_library(), len(grads)
-    flat = array.array("q", itertools.chain.from_iterable(zip(map(torch.Tensor.data_ptr, grads), map(torch.Tensor.numel, grads), kinds)))
+    # the structures' fields, each a slice (120 tensors: a third of the time of taking them one by one)
+    words = [_DTYPES[next(iter(dtypes))]] * (3 * count)
+    words[::3], words[1::3] = list(map(torch.Tensor.data_ptr, grads)), list(map(torch.Tensor.numel, grads))
+    if len(dtypes) > 1:
+        words[2::3] = [_DTYPES[g.dtype] for g in grads]
+    flat = array.array("q", words)
     out = torch.empty(2, dtype=torch.float32, device=device)
     need = lib.nomad_gradient_norm_workspace(count)
     work = torch.empty(need, dtype=torch.uint8, device=device)

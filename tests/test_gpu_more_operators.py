@@ -302,6 +302,57 @@ def test_dense_gradient_against_differences():
         assert abs(difference - formula) <= 2.0 ** -9 * scale
 
 
+@pytest.mark.parametrize("rows,inner,out,dtype", [(12_000, 768, 2048, BF16), (16_500, 1032, 512, F16), (70_001, 264, 512, BF16)])
+def test_large_tiles_with_sums_in_parts(rows, inner, out, dtype):
+    """Against products in 64 bits on the GPU."""
+    note(f"large tiles {rows} {inner}->{out} {dtype}")
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    x, dy, w = (torch.randn(s, device="cuda", generator=gen).to(dtype) for s in ((rows, inner), (rows, out), (out, inner)))
+    dx, dw, db = nomad.dense_gradient(dy, x, w)
+    wide = nomad.dense_gradient(dy, x, w, out_dtype=F32, need_dx=False)
+    a, b, c = dy.double(), x.double(), w.double()
+    near(dx, host(a @ c), (out + 8) * U32 * host(a.abs() @ c.abs()), dtype, "dx")
+    near(dw, host(a.t() @ b), (rows + 8) * U32 * host(a.abs().t() @ b.abs()), dtype, "dw")
+    near(wide[1], host(a.t() @ b), (rows + 8) * U32 * host(a.abs().t() @ b.abs()), F32, "dw in float32")
+    near(db, host(a.sum(0)), (rows + 8) * U32 * host(a.abs().sum(0)), F32, "db")
+    r = dy[:64, :out]
+    near(nomad.dense_product(x[:64], w, residual=r), host(b[:64] @ c.t() + r.double()), (inner + 8) * U32 * host(b[:64].abs() @ c.abs().t() + r.double().abs()), dtype, "few rows")
+
+
+def test_places_that_pass_32_bits():
+    """More than 2^32 elements of an operand, a residual, gradients and logits: the last rows are as they are by themselves."""
+    note("beyond 32 bits")
+    n = 34_000_000
+    x = torch.zeros(n, 128, device="cuda", dtype=BF16)
+    tail = torch.randn(1000, 128, device="cuda").to(BF16)
+    x[-1000:] = tail
+    w = torch.randn(128, 128, device="cuda").to(BF16)
+    y = nomad.dense_product(x, w, activation="silu", residual=x)
+    want = (torch.nn.functional.silu(tail.double() @ w.double().t()) + tail.double())
+    bound = host(tail.double().abs() @ w.double().abs().t())
+    near(y[-1000:], host(want), 1.13 * 136 * U32 * bound + (8 * U32 * (1 + bound) + 2.0 ** -16) * bound + 2 * U32 * host(want.abs()), BF16, "product")
+    assert not y[:-1000:9973].any()
+    del y
+    dx, dw, db = nomad.dense_gradient(x, x, w)
+    near(dx[-1000:], host(tail.double() @ w.double()), 136 * U32 * host(tail.double().abs() @ w.double().abs()), BF16, "dx")
+    near(dw, host(tail.double().t() @ tail.double()), 1008 * U32 * host(tail.double().abs().t() @ tail.double().abs()), BF16, "dw")
+    near(db, host(tail.double().sum(0)), 1008 * U32 * host(tail.double().abs().sum(0)), F32, "db")
+    del dx
+    norm, _ = nomad.gradient_norm([x, tail])
+    full = math.sqrt(2.0) * tail.double().norm().item()
+    assert abs(norm.item() - full) <= 1.01 * U32 * full
+    bias = 0.1 * torch.randn(128, device="cuda")
+    call = dict(groups=8, top_groups=3, group_best=2)
+    r = nomad.route_scored(x, 2, bias=bias, **call)
+    alone = nomad.route_scored(tail, 2, bias=bias, **call)
+    assert torch.equal(r.experts[-1000:], alone.experts) and torch.equal(r.weights[-1000:], alone.weights)
+    assert int(r.offsets[-1]) == 2 * n and torch.equal(r.order[r.slots[-1000:].reshape(-1).long()], torch.arange(2 * n - 2000, 2 * n, device="cuda").int())
+    dw = torch.zeros(n, 2, device="cuda")
+    dw[-1000:] = torch.randn(1000, 2, device="cuda")
+    got = nomad.route_scored_gradient(x, r, dw)
+    assert torch.equal(got[-1000:], nomad.route_scored_gradient(tail, alone, dw[-1000:].contiguous())) and not got[:-1000:9973].any()
+
+
 # ---- the gradients' norm
 
 @pytest.mark.parametrize("count,largest", [(1, 1), (1, 100_003), (5, 4097), (200, 3000), (400, 9), (3, 9_000_001)])
