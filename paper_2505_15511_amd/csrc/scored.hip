@@ -13,7 +13,7 @@ namespace {
 bool is_scoring(const nomad_scoring* s, int32_t n_experts, int32_t k) {
     if (!s || s->struct_size != sizeof(nomad_scoring)) return false;
     if ((s->score != NOMAD_SCORE_SOFTMAX && s->score != NOMAD_SCORE_SIGMOID) || (s->normalize != 0 && s->normalize != 1)) return false;
-    if (!std::isfinite(s->scale) || s->scale == 0.f) return false;
+    if (!std::isfinite(s->scale) || s->scale == 0.f || !std::isfinite(1.f / s->scale)) return false;
     if (s->groups < 1 || s->groups > NOMAD_ROUTE_MAX_GROUPS || n_experts % s->groups || s->top_groups < 1 || s->top_groups > s->groups) return false;
     return (s->group_best == 1 || s->group_best == 2) && k <= (int64_t)s->top_groups * (n_experts / s->groups);
 }

@@ -481,6 +481,33 @@ def test_another_stream_and_graphs():
             assert all(torch.equal(a, b) for a, b in zip(held, fresh))
 
 
+def test_calls_at_once():
+    """Calls on two streams that run side by side, many of them, have nothing in common."""
+    note("calls at once")
+    rng = np.random.default_rng(43)
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    inputs = []
+    for i in range(2):
+        x, w, r = randn((400, 4096), BF16, rng), randn((136, 4096), BF16, rng, 0.02), randn((400, 136), BF16, rng)
+        inputs.append((x, w, r, randn((5000, 128), F32, rng), randn((128,), F32, rng, 0.05)))
+
+    def calls(x, w, r, logits, bias, stream):
+        routing = nomad.route_scored(logits, 4, bias=bias, groups=8, top_groups=3, group_best=2, stream=stream)
+        return (nomad.dense_product(x, w, activation="gelu", residual=r, stream=stream), *nomad.dense_gradient(r, x, w, "silu", r, stream=stream), *routing,
+                nomad.route_scored_gradient(logits, routing, routing.weights, stream=stream), *nomad.gradient_norm([x, w, r, logits], 1.0, stream=stream))
+    want = [calls(*each, None) for each in inputs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i in range(2):
+            with torch.cuda.stream(sides[i]):
+                got[i].append(calls(*inputs[i], None))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for each in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(each, want[i]))
+
+
 def test_clipped_step():
     """The factor goes into the step as it is: the same as gradients that were multiplied by it."""
     rng = np.random.default_rng(42)

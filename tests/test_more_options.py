@@ -33,7 +33,7 @@ def test_scoring(lib):
     for more in ({}, dict(score=0), dict(normalize=0), dict(groups=4, top_groups=1), dict(groups=8, top_groups=2, group_best=2), dict(scale=-2.5), dict(n=0), dict(experts=128, groups=64, top_groups=3)):
         assert all(rc not in (INVALID, TOO_LARGE) for rc in _route(lib, **more)), more
     for more in (dict(size=b.SCORING.size - 8), dict(score=2), dict(normalize=2), dict(groups=3), dict(groups=0), dict(groups=2, top_groups=3), dict(top_groups=0),
-                 dict(group_best=3), dict(group_best=0), dict(scale=0.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(groups=8, top_groups=1), dict(k=9), dict(k=0), dict(dtype=3), dict(n=-1),
+                 dict(group_best=3), dict(group_best=0), dict(scale=0.0), dict(scale=1e-39), dict(scale=float("nan")), dict(scale=float("inf")), dict(groups=8, top_groups=1), dict(k=9), dict(k=0), dict(dtype=3), dict(n=-1),
                  dict(experts=130, groups=65)):
         assert _route(lib, **more) == (INVALID, INVALID), more
     assert _route(lib, experts=16385) == (TOO_LARGE, TOO_LARGE) and _route(lib, n=1 << 31) == (TOO_LARGE, TOO_LARGE)
