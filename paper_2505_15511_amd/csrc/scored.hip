@@ -66,7 +66,7 @@ extern "C" int nomad_route_scored_gradient(const void* logits, int32_t dtype, in
     if (!on.ok()) return NOMAD_E_HIP;
     const bool over_all = scoring->score == NOMAD_SCORE_SOFTMAX && !scoring->normalize;   // (reads the logits)
     const ScoredGradientArgs p{{logits, n, stride, n_experts, k, scoring->normalize, experts, weights, dweights, dlogits},
-                               scoring->scale, scoring->normalize ? 1.f / scoring->scale : 0.f, scoring->score == NOMAD_SCORE_SIGMOID};
+                               scoring->scale, scoring->score == NOMAD_SCORE_SIGMOID};
     const int64_t size = size_of(dtype);
     const bool vec = (!over_all || by(logits, stride, size, 16)) && by(dlogits, n_experts, size, 16);
     hipStream_t st = (hipStream_t)stream;

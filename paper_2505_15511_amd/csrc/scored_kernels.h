@@ -559,7 +559,7 @@ __device__ __forceinline__ float weigh(const T* row, const ScoredArgs& p, int su
         const float most = most_of<LANES>(v);
         if (mine >= 0) share = p.sigmoid ? sigmoid_ratio(v, most) : power_of_e(v - most);
         const float chosen = fold<LANES>(share, [](float a, float b) { return a + b; });
-        if (mine >= 0) share *= __builtin_amdgcn_rcpf(chosen);
+        if (mine >= 0) share /= chosen;   // (of one alone exactly 1)
     } else if (p.sigmoid) {
         if (mine >= 0) share = power_of_e(fminf(v, 0.f)) * __builtin_amdgcn_rcpf(1.f + power_of_e(-fabsf(v)));
     } else if (mine >= 0) {
@@ -702,7 +702,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_scored_small(ScoredArgs p) {
 
 struct ScoredGradientArgs {
     RouteGradientArgs r;
-    float scale, over;         // over: 1 / scale where weights are renormalised, otherwise 0
+    float scale;
     int32_t sigmoid;
 };
 
@@ -729,13 +729,13 @@ __global__ void __launch_bounds__(256) k_scored_gradient(ScoredGradientArgs p) {
         if (j >= p.r.k || expert[j] >= p.r.n_experts) expert[j] = -1;
         weight[j] = expert[j] < 0 ? 0.f : weight[j];
         given[j] = expert[j] < 0 ? 0.f : given[j];
-        inner += weight[j] * given[j];
+        inner += (p.r.normalize ? weight[j] / p.scale : weight[j]) * given[j];   // (a share, exactly 1 of one expert alone, whose gradient is 0)
     }
     T* out = (T*)p.r.dlogits + i * p.r.n_experts;
     if (p.sigmoid || p.r.normalize || expert[0] < 0) {
 #pragma unroll
         for (int j = 0; j < K; ++j) {
-            given[j] = weight[j] * (given[j] - inner * p.over);
+            given[j] = weight[j] * (given[j] - (p.r.normalize ? inner : 0.f));
             if (p.sigmoid && expert[j] >= 0) given[j] /= 1.f + expf(value_of(row[expert[j]]));
         }
         for (int32_t c = sub * epc; c < p.r.n_experts; c += LANES * epc) {
@@ -794,8 +794,8 @@ __global__ void __launch_bounds__(256) k_scored_gradient_rows(ScoredGradientArgs
         if (expert >= p.r.n_experts) expert = -1;
     }
     for (int32_t c = sub; c < chunks; c += 16) held[c] = make_uint4(0, 0, 0, 0);
-    const float inner = fold<16>(expert < 0 ? 0.f : weight * given, [](float a, float b) { return a + b; });
-    float value = weight * (given - inner * p.over);
+    const float inner = fold<16>(expert < 0 || !p.r.normalize ? 0.f : weight / p.scale * given, [](float a, float b) { return a + b; });
+    float value = weight * (given - inner);
     if (expert >= 0 && p.sigmoid) value /= 1.f + expf(value_of(((const T*)p.r.logits)[i * p.r.stride + expert]));
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();

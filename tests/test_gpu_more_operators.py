@@ -118,6 +118,22 @@ def test_scored_strides_and_extremes():
     check_scored(many.neg() * 0.01, 4, 1e4 * torch.randn(16, device="cuda").round(), groups=4, top_groups=2, group_best=2)
 
 
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("scale", [1.0, 2.5, 0.3])
+@pytest.mark.parametrize("n,experts", [(9, 649), (37, 62), (3000, 200)])
+def test_one_expert_alone_has_the_whole_weight(score, scale, n, experts):
+    """Its share is 1 and does not depend on its logit: no rounding is left in either."""
+    note(f"alone {score} {scale} {n} {experts}")
+    rng = np.random.default_rng(n)
+    logits, dw = randn((n, experts), F32, rng, 2.0), randn((n, 1), F32, rng)
+    r = nomad.route_scored(logits, 1, score=score, bias=randn((experts,), F32, rng, 0.1), scale=scale)
+    assert (r.weights == scale).all() and not nomad.route_scored_gradient(logits, r, dw, score=score, scale=scale).any()
+    logits[::2, 1:] = -math.inf                                           # one of three places taken
+    r = nomad.route_scored(logits, 3, score=score, scale=scale)
+    assert (r.weights[::2, 0] == scale).all() and not r.weights[::2, 1:].any()
+    assert not nomad.route_scored_gradient(logits, r, dw.expand(n, 3).contiguous(), score=score, scale=scale)[::2].any()
+
+
 def test_scored_many_rows():
     """Half a million rows against sums in 64 bits: some of them need those."""
     note("scored 500000 x 128")
