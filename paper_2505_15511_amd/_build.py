@@ -24,7 +24,7 @@ HEADERS = [os.path.join(_PKG, "csrc", "nomad_kernels.h"), os.path.join(_PKG, "cs
            os.path.join(_PKG, "csrc", "edge_plan.h"), os.path.join(_PKG, "csrc", "exchange_kernels.h"),
            os.path.join(_PKG, "csrc", "run_kernels.h"), os.path.join(_PKG, "csrc", "field_kernels.h"), os.path.join(_PKG, "csrc", "small_kernels.h"), os.path.join(_PKG, "csrc", "kmeans_plan.h"),
            os.path.join(_PKG, "csrc", "grouped_kernels.h"), os.path.join(_PKG, "csrc", "grouped_launch.h"), os.path.join(_PKG, "csrc", "grouped_plan.h"), os.path.join(_PKG, "csrc", "route_kernels.h"), os.path.join(_PKG, "csrc", "adamw_kernels.h"), os.path.join(_PKG, "csrc", "device_scope.h"),
-           os.path.join(_PKG, "csrc", "route_launch.h"), os.path.join(_PKG, "csrc", "scored_kernels.h"), os.path.join(_PKG, "csrc", "scored_launch.h"), os.path.join(_PKG, "csrc", "norm_kernels.h"),
+           os.path.join(_PKG, "csrc", "route_launch.h"), os.path.join(_PKG, "csrc", "scored_kernels.h"), os.path.join(_PKG, "csrc", "scored_keys.h"), os.path.join(_PKG, "csrc", "scored_launch.h"), os.path.join(_PKG, "csrc", "norm_kernels.h"),
            os.path.join(_PKG, "csrc", "dense_kernels.h"), os.path.join(_PKG, "csrc", "dense_launch.h"), os.path.join(_PKG, "csrc", "dense_plan.h"),
            os.path.join(_ROOT, "include", "nomad.h")]
 

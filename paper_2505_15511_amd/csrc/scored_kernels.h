@@ -18,6 +18,7 @@
 // quarter of the other instructions' rate, are a third of it); 300,000 rows in bfloat16, k = 8 of 4 groups out of 8, 152 us; the gradients 111 (4.7 TB/s written) and 47.
 #pragma once
 #include "route_kernels.h"
+#include "scored_keys.h"
 
 namespace nomad_router {
 
@@ -300,50 +301,6 @@ __device__ __forceinline__ bool choose(const T* row, const ScoredArgs& p, int su
 // number, lower ones larger, so that comparing, sorting and taking the best are one instruction each.  (A step is 2^-24 or 2^-25 of the sums'
 // range.)  Without a bias the step is what is left of a logit's own order, all of it for logits of 16 bits.
 
-__device__ __forceinline__ void order(uint32_t& a, uint32_t& b) {   // the larger first
-    const uint32_t m = a > b ? a : b;
-    b = a > b ? b : a;
-    a = m;
-}
-template <int N>
-__device__ __forceinline__ void bitonic(uint32_t (&v)[N]) {   // a sequence that rises and falls -> descending
-#pragma unroll
-    for (int d = N / 2; d > 0; d /= 2)
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if ((i & d) == 0) order(v[i], v[i + d]);
-}
-template <int N>
-__device__ __forceinline__ void sorted(uint32_t (&v)[N]) {   // descending
-#pragma unroll
-    for (int size = 2; size <= N; size *= 2)
-#pragma unroll
-        for (int d = size / 2; d > 0; d /= 2)
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if ((i & d) == 0) {
-                    if ((i & size) == 0) order(v[i], v[i + d]);
-                    else order(v[i + d], v[i]);
-                }
-}
-// the L largest of N, descending
-template <int L, int N>
-__device__ __forceinline__ void largest(const uint32_t (&v)[N], uint32_t (&out)[L]) {
-#pragma unroll
-    for (int i = 0; i < L; ++i) out[i] = i < N ? v[i] : 0u;
-    sorted(out);
-#pragma unroll
-    for (int at = L; at < N; at += L) {
-        uint32_t more[L];
-#pragma unroll
-        for (int i = 0; i < L; ++i) more[i] = at + i < N ? v[at + i] : 0u;
-        sorted(more);
-#pragma unroll
-        for (int i = 0; i < L; ++i) out[i] = out[i] > more[L - 1 - i] ? out[i] : more[L - 1 - i];
-        bitonic(out);
-    }
-}
-
 __device__ __forceinline__ float power_of_e(float x) {   // for x <= 0, to a unit or two: what rounding x log2(e) loses is put back
     const float power = x * 1.44269504f, rest = fmaf(x, 1.92596303e-8f, fmaf(x, 1.44269504f, -power)), e = __builtin_amdgcn_exp2f(power);
     return x < -150.f ? 0.f : fmaf(e, rest * 0.69314718f, e);
@@ -353,7 +310,6 @@ template <typename T, int CAP, int K, bool VEC, bool GROUPED>
 struct Quick {
     static constexpr int kLanes = 16, kEpc = VEC ? 16 / (int)sizeof(T) : 1, kChunks = CAP / kEpc;
     static constexpr int kBits = CAP == 8 ? 7 : 8;                            // of an expert's number
-    static constexpr int kList = K == 2 ? 4 : 8;                              // a lane keeps: more than it can lose, but for K = 8
     static constexpr float kSteps = (float)((1ull << (32 - kBits)) - 64);     // (rounding takes a key a few steps further)
     struct alignas(VEC ? 16 : sizeof(T)) Chunk { T v[kEpc]; };
     const ScoredArgs& p;
@@ -498,11 +454,8 @@ struct Quick {
         }
 #pragma unroll
         for (int i = 0; i < CAP; ++i) key[i] = v[i] > none ? key[i] : 0u;
-        uint32_t list[kList];
-        largest(key, list);
-        if (GROUPED)
-#pragma unroll
-            for (int i = 0; i < kList; ++i) list[i] = open ? list[i] : 0u;
+        Kept<CAP, K> kept;
+        kept.keep(key, !GROUPED || open);
         // steps within which keys may be in the wrong order
         const uint32_t apart = by_logit ? 0u : (uint32_t)fminf((near + slack) * steps, 1e9f) + 2u;
         const auto same = [&](uint32_t a, uint32_t b) {   // (a key's expert and another's: equal in every bit of logit and bias)
@@ -515,28 +468,14 @@ struct Quick {
         for (int j = 0; j < K; ++j) {
             expert[j] = -1;
             if (j >= p.r.k) continue;
-            const uint32_t best = most_of<kLanes>(list[0]);
-            if (list[0] == best) {
-#pragma unroll
-                for (int i = 0; i + 1 < kList; ++i) list[i] = list[i + 1];
-                list[kList - 1] = best == 0 ? 0u : kList > K ? 0u : 1u;   // 1: something was let go there
-            }
+            const uint32_t best = most_of<kLanes>(kept.list[0]);
+            kept.give(best);
             if (best) expert[j] = (int32_t)(mask - (best & mask));
             if (!exact && best && before && (before >> kBits) - (best >> kBits) <= apart && !same(before, best)) sure = false;
             before = best;
             last = j == p.r.k - 1 ? best : last;
         }
-        if (!exact && last && list[0] && (last >> kBits) - (list[0] >> kBits) <= apart) {
-            bool all = true;
-#pragma unroll
-            for (int i = 0; i < kList; ++i) {
-                const bool close = list[i] != 0 && (last >> kBits) - (list[i] >> kBits) <= apart;
-                all = all && close;
-                if (close && !same(last, list[i])) sure = false;
-            }
-            if (all) sure = false;
-        }
-        if (!exact && kList == K && list[0] == 1u) sure = false;    // (a lane that has given all that it kept)
+        if (!exact && kept.unsure(last, apart, kBits, same)) sure = false;
         return !any_of<kLanes>(!sure, lane);
     }
 };
