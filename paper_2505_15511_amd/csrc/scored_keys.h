@@ -37,9 +37,10 @@ NOMAD_LANE void sorted(uint32_t (&v)[N]) {   // descending
                     else order(v[i + d], v[i]);
                 }
 }
-// the L largest of N, descending
+// the L largest of N, descending; returns the largest of the others (0: there are none)
 template <int L, int N>
-NOMAD_LANE void largest(const uint32_t (&v)[N], uint32_t (&out)[L]) {
+NOMAD_LANE uint32_t largest(const uint32_t (&v)[N], uint32_t (&out)[L]) {
+    uint32_t gone = 0u;
 #pragma unroll
     for (int i = 0; i < L; ++i) out[i] = i < N ? v[i] : 0u;
     sorted(out);
@@ -50,21 +51,27 @@ NOMAD_LANE void largest(const uint32_t (&v)[N], uint32_t (&out)[L]) {
         for (int i = 0; i < L; ++i) more[i] = at + i < N ? v[at + i] : 0u;
         sorted(more);
 #pragma unroll
-        for (int i = 0; i < L; ++i) out[i] = out[i] > more[L - 1 - i] ? out[i] : more[L - 1 - i];
+        for (int i = 0; i < L; ++i) {
+            uint32_t less = more[L - 1 - i];
+            order(out[i], less);
+            gone = less > gone ? less : gone;
+        }
         bitonic(out);
     }
+    return gone;
 }
 
-// The keys that a lane of CAP experts has kept, while up to K of the row are given away, best first
+// The keys that a lane of CAP experts has kept, while up to K of the row are given away, best first.  A lane does not run out of them while it has
+// others: whatever it let go is below the last key given
 template <int CAP, int K>
 struct Kept {
-    static constexpr int kList = K == 2 ? 4 : 8;   // a lane keeps: more than it can lose, but for K = 8
+    static constexpr int kList = K == 2 ? 4 : 8;
     uint32_t list[kList];                          // descending; 0: no key
-    int given;                                     // (a count, not a mark in the list: what is in the list is taken for an expert's key)
+    uint32_t gone;                                 // the largest that found no place in it; 0: all did
 
     NOMAD_LANE void keep(const uint32_t (&key)[CAP], bool open) {
-        largest(key, list);
-        given = 0;
+        gone = largest(key, list);
+        gone = open ? gone : 0u;
 #pragma unroll
         for (int i = 0; i < kList; ++i) list[i] = open ? list[i] : 0u;
     }
@@ -74,24 +81,19 @@ struct Kept {
 #pragma unroll
         for (int i = 0; i + 1 < kList; ++i) list[i] = list[i + 1];
         list[kList - 1] = 0u;
-        given += best != 0;
     }
     // Whether the lane has an expert that may be better than the last one given (0: fewer were given than asked for): one whose key is within `apart` steps, of 2^bits
-    // each, of the last one's, unless same(last, its key)
+    // each, of the last one's, unless same(last, its key).  Of those that it let go it knows the largest alone: that near, it may be any of them
     template <typename F>
     NOMAD_LANE bool unsure(uint32_t last, uint32_t apart, int bits, F same) const {
-        bool may = false;
-        if (last && list[0] && (last >> bits) - (list[0] >> bits) <= apart) {
-            bool all = true;
+        if (last == 0) return false;
+        const auto close = [&](uint32_t key) { return key != 0 && (last >> bits) - (key >> bits) <= apart; };
+        bool may = close(gone);
+        if (close(list[0]))
 #pragma unroll
-            for (int i = 0; i < kList; ++i) {
-                const bool close = list[i] != 0 && (last >> bits) - (list[i] >> bits) <= apart;
-                all = all && close;
-                if (close && !same(last, list[i])) may = true;
-            }
-            if (all) may = true;
-        }
-        return may || (last && kList == K && given == kList);   // (a lane that has given all that it kept)
+            for (int i = 0; i < kList; ++i)
+                if (close(list[i]) && !same(last, list[i])) may = true;
+        return may;
     }
 };
 

@@ -184,7 +184,7 @@ def test_only_experts_of_the_row_are_asked_about(choose, experts, dtype):
     zero, some = np.zeros(experts, np.float32), (1e-3 * rng.integers(0, 3, experts)).astype(np.float32)
     for score, spread, low in (("softmax", 6.0, 0.0), ("softmax", 30.0, 0.0), ("sigmoid", 1.0, -18.0), ("sigmoid", 0.0, -200.0), ("sigmoid", 5.0, 0.0)):
         for k in (1, 2, 3, 8):
-            rows = of(dtype, peaked(rng, 60, experts, spread, low))
+            rows = of(dtype, peaked(rng, 30, experts, spread, low))
             rows[::5, 1:] = -math.inf                                     # fewer than are asked for
             rows[1] = -math.inf
             for bias in (zero, some, None):
@@ -192,3 +192,58 @@ def test_only_experts_of_the_row_are_asked_about(choose, experts, dtype):
                 assert not astray.any(), (score, spread, low, k)
                 if experts % 4 == 0:
                     assert not choose(rows, k, dtype, score, bias, groups=4, top_groups=min(4, 4 * k // experts + 1))[2].any()
+
+
+def right(rows, k, score="sigmoid", bias=None, groups=1, top_groups=1):
+    return mo.route_scored(rows, k, score=score, bias=bias, groups=groups, top_groups=top_groups)[0]
+
+
+def test_what_a_lane_lets_go_may_be_the_best(choose):
+    """As many equal logits in one lane as it keeps, and one more in it that is larger by less than a key holds."""
+    def row(experts, equal, value, at, larger, rest):
+        x = np.full((1, experts), rest, np.float32)
+        x[0, :equal], x[0, at] = value, larger
+        return x
+    up = np.nextafter(np.float32(6.0), np.float32(7.0))
+    for x, k, dtype, biased, want in ((row(128, 4, 1.0, 64, 1 + 2.0 ** -18, 0.0), 1, torch.float32, False, [64]), (row(128, 4, 1.0, 64, 1 + 2.0 ** -18, 0.0), 2, torch.float32, False, [64, 0]),
+                                      (row(64, 4, 20.0, 4, 21.0, 0.0), 2, torch.bfloat16, True, [4, 0]), (row(128, 4, 6.0, 64, up, 0.0), 1, torch.float32, True, [64]),
+                                      (row(256, 4, 1.0, 128, 1 + 2.0 ** -18, 0.0), 3, torch.float32, False, [128, 0, 1])):
+        if k == 3:
+            x[0, [64, 65, 66, 67]] = 1.0                                  # eight in all
+        bias = np.zeros(x.shape[1], np.float32) if biased else None
+        assert right(x, k, bias=bias).tolist() == [want]
+        said, sure, _ = choose(x, k, dtype, bias=bias)
+        assert not sure[0] or said.tolist() == [want], (k, dtype, said)
+
+
+@pytest.mark.parametrize("experts", [50, 64, 128, 200, 256])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+def test_lanes_that_are_sure_are_right(choose, experts, dtype, score):
+    """Rows that repeat one logit, some of them moved by a few units; others saturated or all but zero."""
+    rng = np.random.default_rng(experts)
+    zero, two, some = (np.asarray(b, np.float32) for b in (np.zeros(experts), 0.25 * (np.arange(experts) % 2), 0.02 * rng.normal(size=experts)))
+    kinds = []
+    for value in (1.0, 6.0, 17.0, -9.0):
+        x = np.full((20, experts), value, np.float32)
+        moved = rng.random(x.shape) < np.array([0.02, 0.1, 0.5, 1.0])[rng.integers(0, 4, 20)][:, None]
+        x = np.where(moved, x.view(np.int32) + rng.integers(-200, 201, x.shape), x.view(np.int32)).astype(np.int32).view(np.float32)
+        kinds.append(np.where(rng.random(x.shape) < np.array([0.0, 0.5, 0.9])[rng.integers(0, 3, 20)][:, None], value - 5.0, x).astype(np.float32))
+    kinds += [rng.integers(-3, 4, (20, experts)) * 7.0, peaked(rng, 20, experts, 6.0, 0.0), peaked(rng, 20, experts, 1.0, 30.0)]
+    rows = of(dtype, np.concatenate(kinds))
+    rows[::9, experts // 3:] = -math.inf
+    for bias in (None, zero, two, some):
+        for groups, top in ((1, 1), (4, 2), (2, 1)) if experts % 4 == 0 else ((1, 1),):
+            want = right(rows, 8, score, bias, groups, top)
+            for k in (1, 2, 3, 8):
+                said, sure, _ = choose(rows, k, dtype, score, bias, groups, top)
+                assert np.array_equal(said[sure], want[sure, :k]), (k, groups)
+
+
+@pytest.mark.parametrize("experts,groups,top,k", [(256, 1, 1, 2), (256, 8, 4, 8), (256, 16, 1, 8), (50, 5, 2, 3), (128, 1, 1, 1)])
+def test_lanes_are_sure_of_ordinary_rows(choose, experts, groups, top, k):
+    """Two sums of some hundred in a range of about two are closer than 10^-5 in one of a hundred rows at most; also where one lane has all that is chosen."""
+    rng = np.random.default_rng(experts + k)
+    rows, bias = rng.normal(size=(400, experts)).astype(np.float32), (0.1 * rng.normal(size=experts)).astype(np.float32)
+    said, sure, _ = choose(rows, k, bias=bias, groups=groups, top_groups=top)
+    assert sure.mean() > 0.95 and np.array_equal(said[sure], right(rows, k, bias=bias, groups=groups, top_groups=top)[sure])
