@@ -104,6 +104,7 @@ extern "C" int nomad_dense_product(const nomad_dense_args* args) {
     p.f.y = a.y;
     p.f.y_stride = a.y_stride;
     p.f.activation = a.activation;
+    p.f.factor = 1.f;
     Launch l;
     l.turn = w_kc ? kForward : kTurned;
     l.wide = a.out_dtype != a.dtype;
@@ -150,11 +151,12 @@ extern "C" int nomad_dense_gradient(const nomad_dense_gradient_args* args) {
     const void* dz = a.dy;
     int64_t dz_stride = a.dy_stride;
     char* work = (char*)a.workspace;
+    const float kept = a.dtype == NOMAD_F16 && a.rows > 0 && (a.activation == NOMAD_ACT_SILU || a.activation == NOMAD_ACT_GELU) ? 0.875f : 1.f;   // of dz (k_dense_slope)
     float* db = a.db;   // what the product of the weights' gradient is to leave; with an activation the sums are of dz before its rounding
     if (a.activation != NOMAD_ACT_NONE && a.rows > 0) {
         const SlopePlan l = plan_slope(a.rows, a.out, kPlanUnits);
         const SlopeArgs p{a.dy, a.dy_stride, a.z, a.z_stride, work, a.db ? (l.parts > 1 ? (float*)(work + round16(a.rows * a.out * size)) : a.db) : nullptr,
-                          a.rows, l.length, a.out, a.activation, 0};
+                          a.rows, l.length, a.out, a.activation, 0, kept};
         const bool vec = by(a.dy, a.dy_stride, size, 16) && by(a.z, a.z_stride, size, 16) && a.out % chunk == 0;
         if (a.dtype == NOMAD_F32) slope_f32(p, l.parts, vec, st);
         else if (a.dtype == NOMAD_BF16) slope_bf16(p, l.parts, vec, st);
@@ -174,6 +176,7 @@ extern "C" int nomad_dense_gradient(const nomad_dense_gradient_args* args) {
         p.rows = a.rows;
         p.columns = a.in;
         p.k = a.out;
+        p.f.factor = 1.f / kept;
         p.f.y = a.dx;
         p.f.y_stride = a.dx_stride;
         Launch l;
@@ -195,6 +198,7 @@ extern "C" int nomad_dense_gradient(const nomad_dense_gradient_args* args) {
         p.rows = a.out;
         p.columns = a.in;
         p.k = a.rows;
+        p.f.factor = 1.f / kept;
         p.f.y = a.dw;
         p.f.y_stride = a.in;
         Launch l;

@@ -31,6 +31,7 @@ struct Finish {                  // what follows the sum
     void* y;
     int64_t y_stride;
     int32_t activation;
+    float factor;                // of the sum, without a bias (1: what an operand was kept smaller by)
 };
 struct DenseArgs {
     const void* a;               // A_KC: rows a, k contiguous; otherwise rows k, a contiguous
@@ -176,6 +177,9 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_dense(DenseArgs p) {
                             const int n = r < done_count ? p.columns - col : 0;
 #pragma unroll
                             for (int j = 0; j < N; ++j) v[set][j] = work.at(set, y, j);
+                            if (ACT == kNone && !SLOPE)
+#pragma unroll
+                                for (int j = 0; j < N; ++j) v[set][j] *= p.f.factor;
                             if (SLOPE) {
                                 float z[N];
                                 piece(p.f.slope_at, p.f.slope_stride, r, col, n, z);
@@ -276,6 +280,7 @@ __device__ __forceinline__ float slope_by(int activation, float z) {
 template <typename T, typename O>
 __device__ __forceinline__ void finish_one(const Finish& f, int64_t row, int32_t col, float v) {
     constexpr bool full = sizeof(O) == 4;
+    v *= f.factor;
     if (f.slope_at) v *= slope_by<full>(f.activation, (float)((const T*)f.slope_at)[row * f.slope_stride + col]);
     else {
         if (f.z_out) ((T*)f.z_out)[row * f.z_stride + col] = (T)v;
@@ -399,7 +404,8 @@ static __global__ void __launch_bounds__(256) k_dense_sums(const float* part, in
 }
 
 // dz = dy act'(z), kept in the operands' type, as the products multiply it, and the sums of dz before it is rounded (of the rounded ones a float32 db
-// would be good to 16 bits' rounding only).  A workgroup takes 256 pieces of VEC columns: `wide` side by side, the others in the rows below, and goes
+// would be good to 16 bits' rounding only). Slopes of SiLU and GELU go up to 1.13: in float16 7/8 of dz is kept, which no finite dy takes beyond 65,504, and the products'
+// sums are multiplied by 8/7 (bfloat16 and float32 end where float32 does).  A workgroup takes 256 pieces of VEC columns: `wide` side by side, the others in the rows below, and goes
 // down a run of rows.  Bound by its bytes: 65,536 x 2,048 in bfloat16 150 us (5.4 TB/s).
 struct SlopeArgs {
     const void* dy;
@@ -410,6 +416,7 @@ struct SlopeArgs {
     float* sums;               // [parts][columns], or NULL
     int64_t rows, length;      // rows of a part
     int32_t columns, activation, wide;
+    float factor;              // of dz as it is kept
 };
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) k_dense_slope(SlopeArgs p) {
@@ -433,7 +440,7 @@ __global__ void __launch_bounds__(256) k_dense_slope(SlopeArgs p) {
                 for (int j = 0; j < VEC; ++j) {
                     const float v = (float)g.v[j] * activation_slope<ACT, sizeof(T) == 4>((float)x.v[j]);
                     sum[j] += v;
-                    out.v[j] = (T)v;
+                    out.v[j] = (T)(p.factor * v);
                 }
                 *(Part*)((T*)p.dz + row * p.columns + col) = out;
             }

@@ -72,7 +72,7 @@ void launch_type(const DenseArgs& p, const Launch& l, hipStream_t st) {
     else launch_tile<T, false, false>(p, l, st);
     // (results of one part that are where they belong: nothing is left to do)
     const Finish& f = p.f;
-    const bool done = !p.part || (p.parts == 1 && (const void*)p.part == f.y && !f.bias && !f.residual && !f.slope_at && !f.z_out && f.activation == nomad_grouped::kNone);
+    const bool done = !p.part || (p.parts == 1 && (const void*)p.part == f.y && !f.bias && !f.residual && !f.slope_at && !f.z_out && f.activation == nomad_grouped::kNone && f.factor == 1.f);
     if (!done) {
         if (l.wide) launch_parts<T, float>(p, st);
         else launch_parts<T, T>(p, st);
