@@ -213,8 +213,8 @@ def balance_bias(bias, offsets, rate, stream=None):
     experts = bias.shape[0]
     _whole(bias, "bias", torch.float32, (experts,))
     _whole(offsets, "offsets", torch.int32, (experts + 1,))
-    if not math.isfinite(rate):
-        raise ValueError("rate must be a number")
+    if not abs(rate) <= torch.finfo(torch.float32).max:
+        raise ValueError("rate must be a float32 number")
     out = torch.empty_like(bias)
     st = _stream(device, stream, (bias, offsets, out))
     _check(load_library().nomad_balance_bias(bias.data_ptr(), offsets.data_ptr(), experts, float(rate), out.data_ptr(), device.index, st or None), "nomad_balance_bias")
