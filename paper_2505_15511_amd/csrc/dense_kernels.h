@@ -405,7 +405,8 @@ static __global__ void __launch_bounds__(256) k_dense_sums(const float* part, in
 
 // dz = dy act'(z), kept in the operands' type, as the products multiply it, and the sums of dz before it is rounded (of the rounded ones a float32 db
 // would be good to 16 bits' rounding only). Slopes of SiLU and GELU go up to 1.13: in float16 7/8 of dz is kept, which no finite dy takes beyond 65,504, and the products'
-// sums are multiplied by 8/7 (bfloat16 and float32 end where float32 does).  A workgroup takes 256 pieces of VEC columns: `wide` side by side, the others in the rows below, and goes
+// sums are multiplied by 8/7 (bfloat16 and float32 end where float32 does). db is float32 and has slopes to match: the longer fit of erfc (db of 65,536 rows
+// with GELU good to 2.6e-7, 1.5e-6 with the one for 16-bit results; a call 2 % longer).  A workgroup takes 256 pieces of VEC columns: `wide` side by side, the others in the rows below, and goes
 // down a run of rows.  Bound by its bytes: 65,536 x 2,048 in bfloat16 150 us (5.4 TB/s).
 struct SlopeArgs {
     const void* dy;
@@ -438,7 +439,7 @@ __global__ void __launch_bounds__(256) k_dense_slope(SlopeArgs p) {
                 Part out;
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
-                    const float v = (float)g.v[j] * activation_slope<ACT, sizeof(T) == 4>((float)x.v[j]);
+                    const float v = (float)g.v[j] * activation_slope<ACT, sizeof(T) == 4, true>((float)x.v[j]);
                     sum[j] += v;
                     out.v[j] = (T)(p.factor * v);
                 }

@@ -111,7 +111,7 @@ __device__ __forceinline__ float activate(float z) {
     if (ACT == kGelu) return 0.5f * z * one_plus_erf<FULL>(z, bell<FULL>(z));
     return z;
 }
-template <int ACT, bool FULL>
+template <int ACT, bool FULL, bool TAIL = FULL>   // TAIL: the longer fit of erfc
 __device__ __forceinline__ float activation_slope(float z) {
     if (ACT == kRelu) return z > 0.f ? 1.f : (z != z ? z : 0.f);
     if (ACT == kSilu) {
@@ -120,7 +120,7 @@ __device__ __forceinline__ float activation_slope(float z) {
     }
     if (ACT == kGelu) {
         const float e = bell<FULL>(z);
-        return 0.5f * one_plus_erf<FULL>(z, e) + z * 0.39894228040143268f * e;
+        return 0.5f * one_plus_erf<TAIL>(z, e) + z * 0.39894228040143268f * e;
     }
     return 1.f;
 }
