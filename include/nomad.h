@@ -789,7 +789,8 @@ int nomad_dense_product(const nomad_dense_args* args);
  * Its gradients from dy [rows, out] of `dtype`: with dz = dy act'(z) (z [rows, out] of `dtype`, what the product left in z_out; without an
  * activation dz is dy and z is not looked at)
  *   dx = dz W   [rows, in] of `dtype`;   dw = dz^T x   [out, in] of out_dtype (`dtype` or NOMAD_F32), contiguous;   db = sum of dz   [out] fp32
- * NULL: not asked for (db comes with dw alone).  The residual's gradient is dy.  dz is kept in `dtype`, as the products multiply it.
+ * NULL: not asked for (db comes with dw alone).  The residual's gradient is dy.  dz is kept in `dtype`, as the products multiply
+ * it (finite wherever dy is).
  */
 typedef struct {
   uint32_t struct_size; /* = sizeof(nomad_dense_gradient_args) */
@@ -819,7 +820,7 @@ int nomad_dense_gradient(const nomad_dense_gradient_args* args);
 /*
  * The norm of many tensors together, sqrt of the sum of all their squares times |*grad_scale| (device memory; NULL: 1), and in scale
  * (NULL: not asked for) what a step's gradients have to be multiplied by for a norm of at most max_norm: *grad_scale, times max_norm / norm
- * where the norm is larger (NaN where it is NaN, 0 where it is infinite).  nomad_adamw_step takes it as its grad_scale.  Squares are
+ * where the norm is larger (NaN where it is NaN, 0 where it is infinite: an infinite gradient times 0 is NaN).  nomad_adamw_step takes it as its grad_scale.  Squares are
  * added up in float64, always in the same order.  norm, scale: one fp32 each.  Tensors are contiguous, of any of the three types.
  */
 typedef struct {

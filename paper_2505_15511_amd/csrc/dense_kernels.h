@@ -9,9 +9,9 @@
 // in the same order.
 //
 // What bounds them: the matrix cores, and of a large product what stands beside them: a tile's activation, residual and stores, since a unit
-// holds one workgroup of 256 x 256 and all units finish a tile at about the same time.  65,536 rows of 4,096 -> 4,096 in bfloat16: 1.85 ms by
-// themselves (1,190 TFLOP/s; a plain library product 1.51 to 1.53), 1.97 with bias and GELU, 2.1 with a residual too; dx 1.8, dW 1.8 ms (library 1.7 and
-// 1.9).  Taken back: a wavefront a SIMD with a quarter of a tile and its next operands read ahead (256 sums and 128 operands a lane did not fit
+// holds one workgroup of 256 x 256 and all units finish a tile at about the same time.  65,536 rows of 4,096 -> 4,096 in bfloat16: 1.87 ms by
+// themselves (1,175 TFLOP/s; a plain library product 1.44), 1.97 with bias and GELU, 2.1 with a residual too; dx 1.81, dW 1.78 ms (library 1.65 and
+// 1.82).  Taken back: a wavefront a SIMD with a quarter of a tile and its next operands read ahead (256 sums and 128 operands a lane did not fit
 // the registers), the residual read in the order of the stores, its lines into L2 under the products (both slower).
 #pragma once
 #include "grouped_kernels.h"
@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) k_dense(DenseArgs p) {
                 };
                 // A whole tile with a residual, without z_out: no branches, so that the compiler knows how many loads and stores are on their way, and waits for a piece of
                 // the residual without waiting for the stores behind it (memory operations come back in order). Two rows of pieces are asked for ahead:
-                // 65,536 rows of 768 -> 2,048 in bfloat16 with GELU and a residual 330 us, 366 with one, 335 with three, 368 in the general form.
+                // 65,536 rows of 768 -> 2,048 in bfloat16 with GELU and a residual 325 us, 359 with one, 328 with three, 364 in the general form.
                 const auto finish_whole = [&](auto act) {
                     constexpr int ACT = decltype(act)::value, ahead = 2;
                     struct alignas(sizeof(T)) Piece { T v[N]; } held[ahead][Work::kSets];
@@ -292,7 +292,7 @@ __device__ __forceinline__ void finish_one(const Finish& f, int64_t row, int32_t
 
 // Up to 64 rows, k contiguous on either side: the weights are read once and there are too few tiles for all compute units. A workgroup takes
 // 16 columns and all rows (ROWS sixteens of them), its wavefronts share k, straight from memory to registers, and add up in LDS.  24 rows of
-// 8,192 -> 4,096 in float16: 24.5 us a call, 67 MB of weights at 2.7 TB/s; rows of x come from L2, twice the weights' bytes.
+// 8,192 -> 4,096 in float16: 24.4 us, 67 MB of weights at 2.7 TB/s; rows of x come from L2, twice the weights' bytes.
 template <typename T, typename O, int ROWS>
 __global__ void __launch_bounds__(64 * kFewWaves) k_dense_few(DenseArgs p) {
     constexpr int epc = 16 / (int)sizeof(T), step = 4 * epc;   // k a step: a chunk for every lane group

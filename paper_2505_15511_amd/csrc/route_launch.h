@@ -15,7 +15,7 @@ inline bool by(const void* p, int64_t stride, int64_t size, int64_t bytes) { ret
 // 83 us, 45, 164 and 232 with 256 rows at least)
 inline int64_t chunk_rows(int64_t n) { return std::max<int64_t>(64, (n + 1023) / 1024); }
 // One workgroup does it all where the logits are few (a row of 256: 4.4 us, the three kernels of the other form 12.4; 100 rows of 50: 6.4 against 40)
-// and its counters and slots fit the 64 KB of LDS that a launch has without asking
+// (scored_launch.h has the scored router's times) and its counters and slots fit the 64 KB of LDS that a launch has without asking
 inline bool is_small(int64_t n, int32_t n_experts, int32_t k) { return n * n_experts <= 32768 && n <= 1024 && n_experts + n * k <= 16384; }
 
 // The counts of the chunks into places

@@ -14,8 +14,11 @@
 // k_scored_small     all of it in one workgroup
 // k_scored_gradient_rows, k_scored_gradient   the logits' gradient, made in LDS; of a softmax over all experts, and of rows of more than 512
 //
-// Bound by arithmetic and bytes alike: 500,000 rows of 256 in float32, sigmoid and bias, k = 2: 136 us (3.8 TB/s; exponentials and reciprocals, at a
-// quarter of the other instructions' rate, are a third of it); 300,000 rows in bfloat16, k = 8 of 4 groups out of 8, 152 us; the gradients 111 (4.7 TB/s written) and 47.
+// Bound by arithmetic and bytes alike: 500,000 rows of 256 in float32, sigmoid and bias, k = 2: 142 us (3.6 TB/s; exponentials and reciprocals, at a
+// quarter of the other instructions' rate, are a third of it); 300,000 rows in bfloat16, k = 8 of 4 groups out of 8, 147 us; the gradients 112 (4.7 TB/s written) and 47.
+// Rows for 64 bits cost a wavefront's way each: with a bias of zero and sigmoids that are all but 1 every row is one, and 500,000 of 256 take 1,050 us a call (170 with a bias of
+// 0.02 deviations), 300,000 with k = 8 of groups 1,200 (176); where all logits are the same 1,070 and 1,210.  Over 256 experts, 8,192 rows of 4,096 in float32,
+// k = 2, take 344 us a call by their logits and 515 with a bias, 26 us of bytes.
 #pragma once
 #include "route_kernels.h"
 #include "scored_keys.h"

@@ -40,6 +40,8 @@ void launch_quick(const ScoredArgs& p, bool vec, hipStream_t st) {
 template <typename T>
 void launch_scored(ScoredArgs p, bool vec, hipStream_t st) {
     const int32_t held = held_by_a_lane(p, (int32_t)sizeof(T), vec);
+    // (the line of nomad_route. One workgroup and several kernels, us: 1, 16, 64 and 128 rows of 256 in bfloat16, k = 8 of groups, 14, 20, 36, 63 and 19, 19, 27, 27; in
+    // float32, k = 2, 9, 12, 19, 32 and 15, 15, 18, 19; 1 and 32 rows of 1,024 17, 34 and 27, 89: for up to 256 experts it could lie at some 16 rows)
     const bool small = is_small(p.r.n, p.r.n_experts, p.r.k), quick = !small && held <= 16;
     const int32_t lanes = quick || (small && p.r.n > kSmallThreads / 64 && p.r.n_experts <= 512) ? 16 : 64;
     p.team = team_of(p.groups, lanes);

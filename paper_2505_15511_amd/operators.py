@@ -461,7 +461,8 @@ def combine_gradient(dy, values, slots, weights=None, order=None, need_dvalues=T
 
 def gradient_norm(grads, max_norm=math.inf, grad_scale=None, stream=None):
     """nomad_gradient_norm: (norm, scale), float32 tensors of one element on the GPU: the norm of all tensors together, and the factor that brings it
-    to max_norm at most, as `adamw_step` takes it (grad_scale).  A tensor that is in the list twice counts twice.  grad_scale: None, or a factor that the gradients have yet to be multiplied
+    to max_norm at most, as `adamw_step` takes it (grad_scale).  An infinite gradient makes
+    the factor 0, and is NaN in the step. A tensor that is in the list twice counts twice.  grad_scale: None, or a factor that the gradients have yet to be multiplied
     by, which norm and scale then contain."""
     grads = list(grads)
     if not grads:
