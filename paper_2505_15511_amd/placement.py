@@ -176,7 +176,8 @@ class Placer:
         placer.router.copy_(centres * (4.0 / width))
         placer.router_bias.copy_(centres.pow(2).sum(1) * (-2.0 / width))
         if placer.scoring["score"] == "sigmoid":   # logits of the nearest centres about zero, where scores differ
-            placer.router_bias -= (placer._inputs(X) @ placer.router.t() + placer.router_bias).amax(1).mean()
+            nearest = [(placer._inputs(rows) @ placer.router.t() + placer.router_bias).amax(1) for rows in X.split(1 << 16)]   # (never those of all rows at once)
+            placer.router_bias -= torch.cat(nearest).mean()
         placer.b2.copy_(sums(theta / placer.spread) / count)
         gen = torch.Generator(device=X.device).manual_seed(seed)
         per, losses = max(1, -(-n // batch)), []
